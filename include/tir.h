@@ -53,7 +53,8 @@ typedef enum {
     TIR_ERR_LAUNCH = 4        /* the HIP runtime refused the launch; message holds hipGetErrorString */
 } tir_status;
 
-typedef enum { TIR_F16 = 0, TIR_BF16 = 1, TIR_I8 = 2, TIR_F32 = 3, TIR_I32 = 4 } tir_dtype;
+typedef enum { TIR_F16 = 0, TIR_BF16 = 1, TIR_I8 = 2, TIR_F32 = 3, TIR_I32 = 4,
+               TIR_E4M3 = 5 /* 8-bit floating point, 4 exponent and 3 mantissa bits, largest value 448, no infinity: caches only */ } tir_dtype;
 
 /* Opaque stream handle: pass a hipStream_t (NULL = the default stream). */
 typedef void* tir_stream;
@@ -185,6 +186,61 @@ tir_status tir_conv2d_transpose(const void* x, const void* w, void* y, int64_t N
  */
 tir_status tir_attention(const void* Q, const void* K, const void* V, void* O, int64_t batch, int64_t M, int64_t N,
                          int64_t d, float scale, tir_dtype in, tir_dtype out, tir_stream stream);
+
+/*
+ * A paged cache of keys and values in 8 bits, as a decoder keeps it between calls.  Pools of `blocks` blocks, each of block_tokens = 16, 32,
+ * 64 or 128 tokens of all `heads` key heads; a key or value is the stored 8-bit number (dtype: I8, or E4M3) times the scale
+ * of its block and head.  Every array is dense:
+ *     k [blocks][heads][block_tokens][d]      v [blocks][heads][d][block_tokens]  (a head's values transposed, tokens innermost)
+ *     k_scale, v_scale [blocks][heads] fp32   table [batch][columns] int32
+ * Position j of sequence b is token j % block_tokens of block table[b][j / block_tokens].  d is 64 or 128; k and v are 16-byte aligned.  An entry of
+ * the table outside [0, blocks) is a block that is not there.  columns * block_tokens < 2^31.
+ * The caller owns all of it; the contents of a block that nothing was appended to are never used, nor are those of positions that hold no token.
+ */
+typedef struct tir_kv_cache {
+    void* k;
+    void* v;
+    float* k_scale;
+    float* v_scale;
+    const int32_t* table;
+    int64_t blocks, heads, block_tokens, d, columns;
+    int32_t dtype; /* TIR_I8 or TIR_E4M3 */
+} tir_kv_cache;
+
+/*
+ * Append new tokens to the cache.  Token t of sequence b, head h, is K[b*k_bs + t*k_rs + h*k_hs + c] for c < d (V alike), F16 or BF16, and goes
+ * to position start[b] + t.  start: int32 [batch], the tokens a sequence holds before the call; count: int32 [batch], its new tokens
+ * (NULL: T each).  Both are device arrays, read by the kernel: a negative value counts as 0, a count above T as T; tokens whose position lies beyond the table's columns, or whose
+ * block is not there, are dropped.  Positions that receive no token keep their bytes unless they are held tokens of a block whose scale grows.
+ * For every block and head that receives tokens, with x the new values there, Q = 127 (I8) or 448 (E4M3), and every step one binary32 operation:
+ *     s    = max(s_old, max|x| * (1/Q), 2^-64)         s_old: the block's scale if it holds positions below start[b], else 0; 1/Q rounded to binary32
+ *     q    = round(x * (1/s))                          to the nearest number of the 8-bit type, ties to even, at most Q in magnitude
+ *     held = round(q_held * (s_old * (1/s)))           the block's positions below start[b], which is the identity where s = s_old
+ * A value that is infinite counts as the largest finite one of its sign (of binary32), NaN as 0.
+ * Blocks that receive tokens must belong to one sequence each (two sequences may share blocks that are only read): the result is undefined otherwise.
+ * K and V 16-byte aligned, all strides multiples of 8 elements.  batch = 0 or T = 0 is a no-op.
+ */
+tir_status tir_cache_append(const tir_kv_cache* cache, const void* K, const void* V, const int32_t* start,
+                            const int32_t* count, int64_t batch, int64_t T, int64_t k_bs, int64_t k_rs, int64_t k_hs,
+                            int64_t v_bs, int64_t v_rs, int64_t v_hs, tir_dtype in, tir_stream stream);
+
+/*
+ * Attention of a sequence's newest tokens over the cache.  Sequence b holds lens[b] tokens, of which the last count[b] are asked for (NULL: T
+ * each; both int32 [batch] on the device: values outside [0, columns * block_tokens] resp. [0, T] count as the nearest inside).  Query t < count[b] stands at position
+ * lens[b] - count[b] + t and sees the positions up to its own:
+ *     O[b,t,hq] = sum_j p_j * v_j,  p = softmax over j of scale * (q[b,t,hq] . k_j),  k_j and v_j of key head hq / (Hq / heads)
+ * Q[b*q_bs + t*q_rs + hq*q_hs + c], O alike; heads must divide Hq.  Positions in blocks that are not there are not seen; a query that sees nothing
+ * gives zeros.  Rows t >= count[b] of O are left as they were.  in = F16 or BF16; out = the same type or F32.  scale must be finite.
+ * Scores, softmax and sums are fp32; the 8-bit numbers enter the products unrounded; a probability times the scale of its values is rounded to the input type
+ * relative to the row's largest.  |O - exact| <= 2e-3 * T + 1e-5 with F16, 6e-3 * T + 1e-5 with BF16 (plus 2^-8 * |O| for BF16 output), T = sum_j p_j |v_j|, as for tir_attention.
+ * With a workspace registered for `stream` (tir_set_workspace) few queries over many keys are shared among workgroups, whose results are added in a fixed order; without one
+ * each tile of 32 queries runs on one.
+ * Q and O 16-byte aligned, strides multiples of 8 elements; those of O must keep its rows apart.  batch, T or Hq = 0 is a no-op.
+ */
+tir_status tir_cache_attention(const void* Q, const tir_kv_cache* cache, void* O, const int32_t* lens,
+                               const int32_t* count, int64_t batch, int64_t T, int64_t Hq, int64_t q_bs, int64_t q_rs,
+                               int64_t q_hs, int64_t o_bs, int64_t o_rs, int64_t o_hs, float scale, tir_dtype in,
+                               tir_dtype out, tir_stream stream);
 
 /* Message for the calling thread's last failed call ("" if none).  Never NULL; valid until the
  * thread's next failing call. */

@@ -15,8 +15,8 @@ _PKG = Path(__file__).resolve().parent
 _LIBPATH = _PKG / "libtir.so"
 
 TIR_OK, TIR_ERR_INVALID_ARG, TIR_ERR_UNSUPPORTED, TIR_ERR_ALIGNMENT, TIR_ERR_LAUNCH = range(5)
-TIR_F16, TIR_BF16, TIR_I8, TIR_F32, TIR_I32 = range(5)
-DTYPE_CODES = {"f16": TIR_F16, "bf16": TIR_BF16, "i8": TIR_I8, "f32": TIR_F32, "i32": TIR_I32}
+TIR_F16, TIR_BF16, TIR_I8, TIR_F32, TIR_I32, TIR_E4M3 = range(6)
+DTYPE_CODES = {"f16": TIR_F16, "bf16": TIR_BF16, "i8": TIR_I8, "f32": TIR_F32, "i32": TIR_I32, "e4m3": TIR_E4M3}
 
 EXPORTS = ["tir_gemm", "tir_batch_matmul", "tir_conv2d", "tir_last_error", "tir_gemm_variant",
            "tir_conv2d_variant", "tir_debug_force_tile", "tir_debug_force_variant", "tir_debug_variant_count",
@@ -26,7 +26,7 @@ EXPORTS = ["tir_gemm", "tir_batch_matmul", "tir_conv2d", "tir_last_error", "tir_
            "tir_tune_load", "tir_gemm_fused", "tir_batch_matmul_fused", "tir_conv2d_fused", "tir_attention",
            "tir_conv1d", "tir_conv3d", "tir_conv2d_transpose", "tir_debug_force_ksplit", "tir_debug_fastdiv",
            "tir_conv2d_transpose_variant", "tir_conv3d_variant", "tir_tune_conv3d", "tir_tune_conv2d_transpose",
-           "tir_workspace_bytes", "tir_set_workspace", "tir_gemm_split_static"]
+           "tir_workspace_bytes", "tir_set_workspace", "tir_gemm_split_static", "tir_cache_append", "tir_cache_attention"]
 
 
 class Epilogue(ctypes.Structure):
@@ -39,6 +39,32 @@ def make_epilogue(bias=None, relu=False, scale=0.0, streaming=False):
     if bias is None and not relu and not scale and not streaming:
         return None
     return Epilogue(_ptr(bias) or None, int(bool(relu)), float(scale), int(streaming))
+
+
+class KvCache(ctypes.Structure):
+    """struct tir_kv_cache; make_kv_cache() fills one from tensors, which it keeps alive."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("blocks", ctypes.c_int64), ("heads", ctypes.c_int64), ("block_tokens", ctypes.c_int64), ("d", ctypes.c_int64), ("columns", ctypes.c_int64),
+                ("dtype", ctypes.c_int32)]
+
+
+def make_kv_cache(k, v, k_scale, v_scale, table):
+    """tir_kv_cache of tensors: k [blocks, heads, block_tokens, d] and v [blocks, heads, d, block_tokens] of torch.int8 or torch.float8_e4m3fn,
+    k_scale and v_scale [blocks, heads] float32, table [batch, columns] int32.  The operators change k, v and the scales in place; the tensors may be changed between
+    calls (a table's entries as blocks are handed out), but not replaced."""
+    import torch
+    blocks, heads, tokens, d = k.shape
+    want = [("k", k, (blocks, heads, tokens, d), k.dtype), ("v", v, (blocks, heads, d, tokens), k.dtype), ("k_scale", k_scale, (blocks, heads), torch.float32),
+            ("v_scale", v_scale, (blocks, heads), torch.float32), ("table", table, (table.shape[0], table.shape[-1]), torch.int32)]
+    for name, t, shape, dtype in want:
+        if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous() or t.device != k.device:
+            raise ValueError(f"{name}: a dense {dtype} tensor of {shape} on {k.device} is needed, got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
+    codes = {torch.int8: TIR_I8, torch.float8_e4m3fn: TIR_E4M3}
+    if k.dtype not in codes:
+        raise ValueError(f"k and v: torch.int8 or torch.float8_e4m3fn is needed, got {k.dtype}")
+    cache = KvCache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), table.data_ptr(), blocks, heads, tokens, d, table.shape[1], codes[k.dtype])
+    cache.tensors = (k, v, k_scale, v_scale, table)
+    return cache
 
 
 class TirError(RuntimeError):
@@ -57,6 +83,7 @@ def _load_native():
     lib()
     from . import _native as module
     module.set_epilogue_type(Epilogue)
+    module.set_cache_type(KvCache)
     _native = module
     return module
 
@@ -128,6 +155,11 @@ def lib() -> ctypes.CDLL:
     L.tir_conv2d_transpose.restype = ci
     L.tir_attention.argtypes = [vp, vp, vp, vp] + [i64] * 4 + [ctypes.c_float, ci, ci, vp]
     L.tir_attention.restype = ci
+    pc = ctypes.POINTER(KvCache)
+    L.tir_cache_append.argtypes = [pc] + [vp] * 4 + [i64] * 8 + [ci, vp]
+    L.tir_cache_append.restype = ci
+    L.tir_cache_attention.argtypes = [vp, pc, vp, vp, vp] + [i64] * 9 + [ctypes.c_float, ci, ci, vp]
+    L.tir_cache_attention.restype = ci
     L.tir_tune_batch_matmul.argtypes = [vp, vp, vp] + [i64] * 13 + [ci, ci, pe, ci, pd, vp]
     L.tir_tune_batch_matmul.restype = ci
     L.tir_tune_conv2d.argtypes = [vp, vp, vp] + [i64] * 7 + [ci] * 7 + [ci, ci, pe, ci, pd, vp]
@@ -385,6 +417,33 @@ def tir_attention_status(Q, K, V, O, batch, M, N, d, scale, in_dtype, out_dtype,
 def tir_attention(Q, K, V, O, batch, M, N, d, scale, in_dtype, out_dtype, stream=None) -> None:
     """O[b] = softmax(scale * Q[b] K[b]^T) V[b]; Q [batch, M, d], K and V [batch, N, d], d in (64, 128)."""
     st = (_native or _load_native()).tir_attention(Q, K, V, O, batch, M, N, d, scale, in_dtype, out_dtype, stream)
+    if st:
+        _check(st)
+
+
+def _cache_arg(cache):
+    return None if cache is None else ctypes.byref(cache)
+
+
+def tir_cache_append_status(cache, K, V, start, count, batch, T, k_bs, k_rs, k_hs, v_bs, v_rs, v_hs, in_dtype, stream=0) -> int:
+    return lib().tir_cache_append(_cache_arg(cache), _ptr(K), _ptr(V), _ptr(start), _ptr(count), batch, T, k_bs, k_rs, k_hs, v_bs, v_rs, v_hs, _code(in_dtype), stream)
+
+
+def tir_cache_append(cache, K, V, start, count, batch, T, k_bs, k_rs, k_hs, v_bs, v_rs, v_hs, in_dtype, stream=None) -> None:
+    """Token t of sequence b to position start[b] + t of its blocks; start and count (None: T each): int32 device tensors [batch]."""
+    st = (_native or _load_native()).tir_cache_append(cache, K, V, start, count, batch, T, k_bs, k_rs, k_hs, v_bs, v_rs, v_hs, in_dtype, stream)
+    if st:
+        _check(st)
+
+
+def tir_cache_attention_status(Q, cache, O, lens, count, batch, T, Hq, q_bs, q_rs, q_hs, o_bs, o_rs, o_hs, scale, in_dtype, out_dtype, stream=0) -> int:
+    return lib().tir_cache_attention(_ptr(Q), _cache_arg(cache), _ptr(O), _ptr(lens), _ptr(count), batch, T, Hq, q_bs, q_rs, q_hs, o_bs, o_rs, o_hs, float(scale),
+                                     _code(in_dtype), _code(out_dtype), stream)
+
+
+def tir_cache_attention(Q, cache, O, lens, count, batch, T, Hq, q_bs, q_rs, q_hs, o_bs, o_rs, o_hs, scale, in_dtype, out_dtype, stream=None) -> None:
+    """The newest count[b] (None: T) of the lens[b] tokens of sequence b over the cache, each up to its own position."""
+    st = (_native or _load_native()).tir_cache_attention(Q, cache, O, lens, count, batch, T, Hq, q_bs, q_rs, q_hs, o_bs, o_rs, o_hs, scale, in_dtype, out_dtype, stream)
     if st:
         _check(st)
 

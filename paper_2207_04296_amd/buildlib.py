@@ -19,6 +19,7 @@ OBJ = PKG / "_build"
 LIB = PKG / "libtir.so"
 NATIVE = PKG / "_native.so"
 N_UNITS = 6
+UNITS = ["tir_cache"]      # the decoder's attentions: one translation unit each
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-but-set-variable",
@@ -91,6 +92,7 @@ def build(verbose: bool = True, jobs: int | None = None, defines=(), lib: Path =
     extra = [f"-D{d}" for d in defines]
     jobs_list = [(CSRC / "tir_api.hip", OBJ / f"tir_api{tag}.o", extra),
                  (CSRC / "tir_attn.hip", OBJ / f"tir_attn{tag}.o", extra)]
+    jobs_list += [(CSRC / f"{u}.hip", OBJ / f"{u}{tag}.o", extra) for u in UNITS]
     for u in range(N_UNITS):
         jobs_list.append((CSRC / "tir_inst.hip", OBJ / f"tir_inst{u}{tag}.o", [f"-DTIR_UNIT={u}"] + extra))
     with ThreadPoolExecutor(max_workers=jobs or min(8, os.cpu_count() or 1)) as ex:

@@ -6,7 +6,8 @@
 // (3.0 us for the same call, 2.3 of them the HIP launch).
 //
 // Conversions by C parameter type: pointers take a tensor (its data_ptr()), an integer address or None; tir_dtype a
-// code or a name ("f16", ...); const tir_epilogue* None or an instance of the binding's Epilogue (set_epilogue_type); the last argument, the
+// code or a name ("f16", ...); const tir_epilogue* None or an instance of the binding's Epilogue (set_epilogue_type), const tir_kv_cache* an instance of
+// its KvCache (set_cache_type); the last argument, the
 // stream, None (torch's current stream), an integer handle or an object with .cuda_stream.  Every function returns the
 // tir_status as an int; wrong argument types raise.
 #define PY_SSIZE_T_CLEAN
@@ -26,7 +27,8 @@ PyObject* g_cuda_stream = nullptr;
 PyObject* g_current_stream = nullptr; // torch.cuda.current_stream: initialises the device, used for the first None
 PyObject* g_get_device = nullptr;     // torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 PyObject* g_raw_stream = nullptr;
-PyObject* g_epilogue_type = nullptr;  // the ctypes structure that mirrors tir_epilogue
+PyObject* g_epilogue_type = nullptr;  // the ctypes structures that mirror tir_epilogue and tir_kv_cache
+PyObject* g_cache_type = nullptr;
 bool g_cuda_ready = false;
 
 bool to_address(PyObject* o, void** out) {
@@ -70,7 +72,7 @@ bool to_stream(PyObject* o, void** out) {
     return !(*out == nullptr && PyErr_Occurred());
 }
 
-// One converter per C parameter type; `view` keeps an epilogue's buffer until the call has returned.
+// One converter per C parameter type; `view` keeps a structure's buffer until the call has returned (no entry point takes two).
 struct Held {
     Py_buffer view;
     bool used = false;
@@ -102,7 +104,7 @@ bool convert(PyObject* o, float* out, Held&) {
 bool convert(PyObject* o, tir_dtype* out, Held& h) {
     if (PyUnicode_Check(o)) {
         static const struct { const char* name; tir_dtype code; } kNames[] = {
-            {"f16", TIR_F16}, {"bf16", TIR_BF16}, {"i8", TIR_I8}, {"f32", TIR_F32}, {"i32", TIR_I32}};
+            {"f16", TIR_F16}, {"bf16", TIR_BF16}, {"i8", TIR_I8}, {"f32", TIR_F32}, {"i32", TIR_I32}, {"e4m3", TIR_E4M3}};
         for (const auto& k : kNames)
             if (PyUnicode_CompareWithASCIIString(o, k.name) == 0) {
                 *out = k.code;
@@ -116,25 +118,29 @@ bool convert(PyObject* o, tir_dtype* out, Held& h) {
     *out = (tir_dtype)v;
     return true;
 }
-bool convert(PyObject* o, const tir_epilogue** out, Held& h) {
+// A structure that the binding declares; None is a null pointer.
+template <class S> bool convert_struct(PyObject* o, const S** out, Held& h, PyObject* type, const char* what, const char* name) {
     *out = nullptr;
     if (o == Py_None) return true;
     // (any object has a buffer that could be read as the struct: a bias array's first values would become its address)
-    const int is = g_epilogue_type ? PyObject_IsInstance(o, g_epilogue_type) : 0;
+    const int is = type ? PyObject_IsInstance(o, type) : 0;
     if (is < 0) return false;
     if (!is) {
-        PyErr_Format(PyExc_TypeError, "epilogue: expected an Epilogue or None, got %.200s", Py_TYPE(o)->tp_name);
+        PyErr_Format(PyExc_TypeError, "%s: expected an %s or None, got %.200s", what, name, Py_TYPE(o)->tp_name);
         return false;
     }
     if (PyObject_GetBuffer(o, &h.view, PyBUF_SIMPLE) != 0) return false;
     h.used = true;
-    if ((size_t)h.view.len < sizeof(tir_epilogue)) {
-        PyErr_SetString(PyExc_ValueError, "epilogue: the buffer is smaller than tir_epilogue");
+    if ((size_t)h.view.len < sizeof(S)) {
+        PyErr_Format(PyExc_ValueError, "%s: the buffer is smaller than the structure", what);
         return false;
     }
-    *out = (const tir_epilogue*)h.view.buf;
+    *out = (const S*)h.view.buf;
     return true;
 }
+bool convert(PyObject* o, const tir_epilogue** out, Held& h) { return convert_struct(o, out, h, g_epilogue_type, "epilogue", "Epilogue"); }
+bool convert(PyObject* o, const tir_kv_cache** out, Held& h) { return convert_struct(o, out, h, g_cache_type, "cache", "instance of KvCache"); }
+bool convert(PyObject* o, const int32_t** out, Held&) { return to_address(o, (void**)out); }
 
 template <class... A, size_t... I>
 PyObject* invoke(tir_status (*fn)(A...), PyObject* const* args, std::index_sequence<I...>) {
@@ -171,23 +177,27 @@ TIR_PY(tir_conv1d)
 TIR_PY(tir_conv3d)
 TIR_PY(tir_conv2d_transpose)
 TIR_PY(tir_attention)
+TIR_PY(tir_cache_append)
+TIR_PY(tir_cache_attention)
 #undef TIR_PY
 
-// set_epilogue_type(cls): called once by the binding, before any operator.
-PyObject* py_set_epilogue_type(PyObject*, PyObject* cls) {
+// set_epilogue_type(cls), set_cache_type(cls): called once by the binding, before any operator.
+PyObject* set_type(PyObject* cls, PyObject** type) {
     if (!PyType_Check(cls)) {
-        PyErr_SetString(PyExc_TypeError, "set_epilogue_type: expected a class");
+        PyErr_SetString(PyExc_TypeError, "expected a class");
         return nullptr;
     }
     Py_INCREF(cls);
-    Py_XSETREF(g_epilogue_type, cls);
+    Py_XSETREF(*type, cls);
     Py_RETURN_NONE;
 }
+PyObject* py_set_epilogue_type(PyObject*, PyObject* cls) { return set_type(cls, &g_epilogue_type); }
+PyObject* py_set_cache_type(PyObject*, PyObject* cls) { return set_type(cls, &g_cache_type); }
 
 #define TIR_METHOD(fn) {#fn, (PyCFunction)(void (*)(void))py_##fn, METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {TIR_METHOD(tir_gemm_fused), TIR_METHOD(tir_batch_matmul_fused), TIR_METHOD(tir_conv2d_fused), TIR_METHOD(tir_conv1d),
-                          TIR_METHOD(tir_conv3d), TIR_METHOD(tir_conv2d_transpose), TIR_METHOD(tir_attention),
-                          {"set_epilogue_type", py_set_epilogue_type, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                          TIR_METHOD(tir_conv3d), TIR_METHOD(tir_conv2d_transpose), TIR_METHOD(tir_attention), TIR_METHOD(tir_cache_append), TIR_METHOD(tir_cache_attention),
+                          {"set_epilogue_type", py_set_epilogue_type, METH_O, nullptr}, {"set_cache_type", py_set_cache_type, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
 PyObject* attribute(const char* module, const char* name) {

@@ -16,6 +16,7 @@
 #include "tir.h"
 #include "tir_launch.h"
 #include "tir_attention.h"
+#include "tir_host.h"
 #include "tir_depthwise.h"
 
 namespace tir {
@@ -154,6 +155,14 @@ static tir_status fail(tir_status st, const char* fmt, ...) {
     return st;
 }
 
+tir_status host_error(tir_status st, const char* fmt, ...) {
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_err, sizeof g_err, fmt, ap);
+    va_end(ap);
+    return st;
+}
+
 static const int64_t kMaxExtent = 2147483647LL;
 static const double kCUs = 256.0;
 
@@ -261,6 +270,19 @@ static SplitLimits stream_split_limits(hipStream_t stream) {
     }
     std::lock_guard<std::mutex> lock(g_ws_mu);
     return g_ws.count(std::make_pair(dev, stream)) ? kRegisteredSplit : kNoSplit;
+}
+
+StreamWorkspace stream_workspace(hipStream_t stream) {
+    const StreamWorkspace none = {nullptr, nullptr, 0, 0};
+    if (!g_any_ws.load(std::memory_order_acquire)) return none;
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess) {
+        (void)hipGetLastError();
+        return none;
+    }
+    std::lock_guard<std::mutex> lock(g_ws_mu);
+    auto it = g_ws.find(std::make_pair(dev, stream));
+    return it == g_ws.end() ? none : StreamWorkspace{it->second.partial, it->second.count, kWsBytes, kWsTiles};
 }
 
 // The kernels divide by these launch constants through multiply-and-shift (see Params); a GEMM divides by one of them.

@@ -1,0 +1,574 @@
+// A paged cache of keys and values in 8 bits, and attention over it.
+//
+// Pools of blocks of T tokens (T = 16, 32, 64 or 128), one [T][d] tile of keys and one [d][T] tile of values per block and head, each with
+// a scale of its own; a table gives every sequence its blocks.  The values' tiles are transposed because the second product of an
+// attention, O^T = V^T P^T, contracts over the tokens: a lane's operand is 16 tokens of one channel, which is one 16-byte load this way.
+#pragma once
+#include "tir_kernel.h"
+
+namespace tir {
+
+enum : int { CT_I8 = 0, CT_E4M3 = 1 };
+
+struct CacheView {
+    char* k;                // [blocks][heads][T][d]
+    char* v;                // [blocks][heads][d][T]
+    float* ks;              // [blocks][heads]
+    float* vs;
+    const int* table;       // [batch][cols]
+    int blocks, heads, cols, shift;      // T = 1 << shift
+};
+
+struct AppendParams {
+    CacheView c;
+    const void* K;          // new tokens: element (sequence, token, head, channel) at b*bs + t*rs + h*hs + channel
+    const void* V;
+    long long k_bs, k_rs, k_hs, v_bs, v_rs, v_hs;
+    const int* start;       // tokens a sequence holds already
+    const int* count;       // new tokens of a sequence, at most T; null: T each
+    int T, touched;         // touched: blocks that T tokens can reach into
+    unsigned div_h_magic, div_t_magic;      // / heads, / touched
+    int div_h_shift, div_t_shift;
+};
+
+struct CacheAttnParams {
+    CacheView c;
+    const void* Q;
+    void* O;
+    long long q_bs, q_rs, q_hs, o_bs, o_rs, o_hs;
+    const int* lens;        // tokens a sequence holds, the new ones among them
+    const int* count;       // its queries, at most T; null: T each
+    int T, G;               // query heads per key head
+    int batch, tiles;       // tiles of queries per sequence and key head
+    int slices;             // workgroups that share a tile's keys
+    int out32;              // fp32 output
+    float scale_log2e;
+    void* ws;               // partial results: [tile][slice][kPartial] (slices > 1)
+    unsigned* ws_count;     // [tile], zero between launches
+    unsigned div_g_magic, div_h_magic, div_tiles_magic;      // / G, / heads, / tiles
+    int div_g_shift, div_h_shift, div_tiles_shift;
+};
+
+hipError_t launch_append(const AppendParams& p, int dt, int ct, int d, int64_t batch, hipStream_t stream);
+hipError_t launch_cache_attention(const CacheAttnParams& p, int dt, int ct, int d, hipStream_t stream);
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
+// ---------------------------------------------------------------------------------------------
+// Appending.
+//
+// Of a block and head that gets tokens: s = max(scale it has (0 if it holds no earlier token of the sequence), max|x| * (1/Q), 2^-64), Q the
+// largest value of the 8-bit type; the new values are x * (1/s) rounded to that type, and where s grew the held ones are
+// rounded again from q * (s_old * (1/s)).  Every operation is one binary32 operation, so that the result is one defined value.
+// A value that is not finite counts as the nearest finite one, NaN as 0.
+//
+// One workgroup per sequence, block it reaches into, head, and keys or values: the scale needs all of the block's new values first.  They stay in
+// registers between the two.  Bound by memory (2 bytes read and 1 written per value), for single tokens by latency.
+// ---------------------------------------------------------------------------------------------
+template <int CT> __device__ __forceinline__ float cache_step() { return CT == CT_I8 ? (float)(1.0 / 127.0) : (float)(1.0 / 448.0); }
+
+// Four values, already times 1/s, as the bytes of a word.
+template <int CT> __device__ __forceinline__ unsigned to_eight(float a, float b, float c, float d) {
+    constexpr float top = CT == CT_I8 ? 127.0f : 448.0f;
+    if constexpr (CT == CT_I8) {
+        auto one = [](float x) __attribute__((always_inline)) { return (unsigned)(int)__builtin_amdgcn_fmed3f(__builtin_rintf(x), -top, top) & 255u; };
+        return one(a) | one(b) << 8 | one(c) << 16 | one(d) << 24;
+    } else {
+        auto one = [](float x) __attribute__((always_inline)) { return __builtin_amdgcn_fmed3f(x, -top, top); };
+        const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(one(a), one(b), 0, false);
+        return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(one(c), one(d), lo, true);
+    }
+}
+// Bytes I of a word as a value.
+template <int CT> __device__ __forceinline__ void from_eight(unsigned w, float (&f)[4]) {
+    if constexpr (CT == CT_I8) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = (float)(signed char)(w >> (8 * i));
+    } else {
+        typedef float f2 __attribute__((ext_vector_type(2)));
+        const f2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+        f[0] = lo[0]; f[1] = lo[1]; f[2] = hi[0]; f[3] = hi[1];
+    }
+}
+template <int CT> __device__ __forceinline__ unsigned requantise(unsigned w, float ratio) {
+    float f[4];
+    from_eight<CT>(w, f);
+    return to_eight<CT>(f[0] * ratio, f[1] * ratio, f[2] * ratio, f[3] * ratio);
+}
+// Eight 16-bit values as finite floats.
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+template <int DT> __device__ __forceinline__ f32x8 finite8(const uint4& w) {
+    f32x8 f;
+    auto put = [&](int i, unsigned h) __attribute__((always_inline)) {
+        float x;
+        if constexpr (DT == DT_F16) x = (float)__builtin_bit_cast(_Float16, (unsigned short)h);
+        else x = __builtin_bit_cast(float, h << 16);
+        x = x == x ? x : 0.f;
+        f[i] = __builtin_amdgcn_fmed3f(x, -__FLT_MAX__, __FLT_MAX__);
+    };
+    put(0, w.x & 0xffffu); put(1, w.x >> 16); put(2, w.y & 0xffffu); put(3, w.y >> 16);
+    put(4, w.z & 0xffffu); put(5, w.z >> 16); put(6, w.w & 0xffffu); put(7, w.w >> 16);
+    return f;
+}
+
+constexpr int kAppendThreads = 256;
+
+template <int DT, int CT, int DH, bool KEYS> __device__ __forceinline__ void append_side(const AppendParams& p) {
+    const int bj = (int)fastdiv(blockIdx.x, p.div_h_magic, p.div_h_shift);
+    const int h = (int)blockIdx.x - bj * p.c.heads;
+    const int b = (int)fastdiv((unsigned)bj, p.div_t_magic, p.div_t_shift);
+    const int j = bj - b * p.touched;
+    const int bt = 1 << p.c.shift;
+    float* scale = KEYS ? p.c.ks : p.c.vs;
+    const long long rs = 2 * (KEYS ? p.k_rs : p.v_rs);
+    // positions lo .. hi - 1 of the sequence are this block's new tokens
+    int start = p.start[b], cnt = p.count ? p.count[b] : p.T;
+    start = start < 0 ? 0 : start;
+    cnt = cnt < 0 ? 0 : (cnt > p.T ? p.T : cnt);
+    const long long col = (long long)(start >> p.c.shift) + j;
+    if (col >= p.c.cols) return;
+    const long long first = col << p.c.shift;
+    const int lo = first > start ? 0 : (int)(start - first);                       // in the block
+    const long long left = (long long)start + cnt - first;
+    const int hi = left >= bt ? bt : (int)(left < 0 ? 0 : left);
+    if (hi <= lo) return;
+    const int id = p.c.table[(long long)b * p.c.cols + col];
+    if (id < 0 || id >= p.c.blocks) return;
+    const long long bh = (long long)id * p.c.heads + h;
+    scale += bh;
+    char* const tile = (KEYS ? p.c.k : p.c.v) + ((bh * DH) << p.c.shift);
+    // (token 0 of the block, which need not be a new one)
+    const char* const src = (const char*)(KEYS ? p.K : p.V) + 2 * (b * (KEYS ? p.k_bs : p.v_bs) + h * (KEYS ? p.k_hs : p.v_hs)) + (first - start) * rs;
+
+    // A thread's units.  Keys: 16 channels of one token, so that rows are read and written whole.  Values: 8 channels of 4 tokens, which are
+    // one word of each of 8 of the tile's rows.  Either is two to four 16-byte loads, and 128 tokens of 128 channels are four or two units per thread.
+    constexpr int UK = 128 * DH / 16 / kAppendThreads, UV = 128 / 4 * DH / 8 / kAppendThreads;
+    constexpr int KC = DH / 16;
+    uint4 w[2 * UK];
+    static_assert(2 * UK == 4 * UV, "");
+    if constexpr (KEYS) {
+#pragma unroll
+        for (int u = 0; u < UK; ++u) {
+            const int q = (int)threadIdx.x + u * kAppendThreads, tok = q / KC, c = q % KC;
+            const bool in = tok >= lo && tok < hi;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) w[2 * u + e] = in ? *(const uint4*)(src + tok * rs + c * 32 + e * 16) : make_uint4(0, 0, 0, 0);
+        }
+    } else {
+#pragma unroll
+        for (int u = 0; u < UV; ++u) {
+            const int q = (int)threadIdx.x + u * kAppendThreads, grp = q & (bt / 4 - 1), c = q >> (p.c.shift - 2);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int tok = grp * 4 + e;
+                w[4 * u + e] = tok >= lo && tok < hi && c < DH / 8 ? *(const uint4*)(src + tok * rs + c * 16) : make_uint4(0, 0, 0, 0);
+            }
+        }
+    }
+    float was = 0.f;
+    if (lo > 0) was = *scale;
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < 2 * UK; ++i) {
+        const f32x8 f = finite8<DT>(w[i]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = __builtin_fmaxf(top, __builtin_fabsf(f[e]));
+    }
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) top = __builtin_fmaxf(top, __shfl_xor(top, s));
+    __shared__ float tops[kAppendThreads / 64];
+    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+    __syncthreads();                                     // (everybody has read the old scale, too)
+#pragma unroll
+    for (int i = 0; i < kAppendThreads / 64; ++i) top = __builtin_fmaxf(top, tops[i]);
+    float now = top * cache_step<CT>();
+    now = __builtin_fmaxf(now, 0x1p-64f);
+    now = __builtin_fmaxf(now, was);
+    const float inv = 1.0f / now;
+    const float ratio = was * inv;
+    const bool grew = now > was && lo > 0;
+    if (threadIdx.x == 0 && now != was) *scale = now;
+
+    if constexpr (KEYS) {
+#pragma unroll
+        for (int u = 0; u < UK; ++u) {
+            const int q = (int)threadIdx.x + u * kAppendThreads, tok = q / KC, c = q % KC;
+            uint4* const dst = (uint4*)(tile + tok * DH + c * 16);
+            if (tok >= lo && tok < hi) {
+                const f32x8 f = finite8<DT>(w[2 * u]), e = finite8<DT>(w[2 * u + 1]);
+                *dst = make_uint4(to_eight<CT>(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv), to_eight<CT>(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv),
+                                  to_eight<CT>(e[0] * inv, e[1] * inv, e[2] * inv, e[3] * inv), to_eight<CT>(e[4] * inv, e[5] * inv, e[6] * inv, e[7] * inv));
+            } else if (grew && tok < lo) {
+                const uint4 t = *dst;
+                *dst = make_uint4(requantise<CT>(t.x, ratio), requantise<CT>(t.y, ratio), requantise<CT>(t.z, ratio), requantise<CT>(t.w, ratio));
+            }
+        }
+    } else {
+#pragma unroll
+        for (int u = 0; u < UV; ++u) {
+            const int q = (int)threadIdx.x + u * kAppendThreads, grp = q & (bt / 4 - 1), c = q >> (p.c.shift - 2);
+            const int t0 = grp * 4;
+            if (c < DH / 8 && t0 < hi && (t0 + 4 > lo || grew)) {
+                // bytes of the word that are new, and that are held
+                unsigned fresh = 0, held = 0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (t0 + e >= lo && t0 + e < hi) fresh |= 255u << (8 * e);
+                    if (t0 + e < lo) held |= 255u << (8 * e);
+                }
+                char* const dst = tile + ((c * 8) << p.c.shift) + t0;
+                const f32x8 f0 = finite8<DT>(w[4 * u]), f1 = finite8<DT>(w[4 * u + 1]), f2 = finite8<DT>(w[4 * u + 2]), f3 = finite8<DT>(w[4 * u + 3]);
+                const unsigned again = grew ? held : 0u;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    unsigned* const at = (unsigned*)(dst + (i << p.c.shift));
+                    const unsigned o = to_eight<CT>(f0[i] * inv, f1[i] * inv, f2[i] * inv, f3[i] * inv);
+                    if (fresh == ~0u) {
+                        *at = o;
+                    } else {
+                        const unsigned was8 = *at, kept = (was8 & ~again) | (requantise<CT>(was8, ratio) & again);
+                        *at = (kept & ~fresh) | (o & fresh);
+                    }
+                }
+            }
+        }
+    }
+}
+
+template <int DT, int CT, int DH> __global__ void __launch_bounds__(kAppendThreads) cache_append_kernel(const AppendParams p) {
+    if (blockIdx.y == 0) append_side<DT, CT, DH, true>(p);
+    else append_side<DT, CT, DH, false>(p);
+}
+
+// ---------------------------------------------------------------------------------------------
+// Attention over the cache.
+//
+// S^T = K Q^T and O^T = V^T P^T on 32x32x16 MFMAs as in the dense attention, one lane per query.  A key head's query heads and a
+// sequence's new tokens share the tile of 32 rows: row t*G + g is token t of query head h*G + g.  Row i of the first operand may be any key, and the one
+// taken is 16*((i>>2)&1) + 4*(i>>3) + (i&3): the lane of half-wave g then holds the scores of the 16 consecutive keys from 16*g, which are
+// the tokens of one scale, and of one 16-byte load of a row of the values' tile.
+//
+// 8-bit values are exact in 16 bits, so the operands are converted as they are and the scales enter elsewhere: the keys' in the score (t = q.k * scale *
+// ks, one factor per lane and chunk), the values' in the weight: w_j = p_j * vs_j is what is rounded for the second product, and the softmax runs on t_j + log2(vs_j), so that
+// the largest weight of a row is one number whatever the scales are (p_j * vs_j with a p of at most 1 would leave binary16's normal range): 1, or 2^14 in binary16, which
+// then holds weights down to 2^-28 of the largest to eleven bits; relative to 1 they would end at 2^-14, and a hundred thousand small weights rounded alike are seen in the sum.  The sum of probabilities takes each weight over its
+// scale again: l = sum w_j / vs_j, in fp32.
+// ---------------------------------------------------------------------------------------------
+template <int DT, int CT> __device__ __forceinline__ uint2 widen(unsigned w) {
+    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    if constexpr (CT == CT_E4M3 && DT == DT_F16) {
+        return make_uint2(__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false)),
+                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true)));
+    } else if constexpr (CT == CT_E4M3) {
+        return make_uint2(__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false)),
+                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true)));
+    } else if constexpr (DT == DT_F16) {
+        // x + 128 as the low bits of 1024 + x + 128 in binary16, less 1152
+        const unsigned x = w ^ 0x80808080u;
+        const h2 off = {(_Float16)1152.f, (_Float16)1152.f};
+        return make_uint2(__builtin_bit_cast(unsigned, __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, x, 0x07010700u)) - off),
+                          __builtin_bit_cast(unsigned, __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, x, 0x07030702u)) - off));
+    } else {
+        float f[4];
+        from_eight<CT>(w, f);
+        const b2 lo = {(__bf16)f[0], (__bf16)f[1]}, hi = {(__bf16)f[2], (__bf16)f[3]};
+        return make_uint2(__builtin_bit_cast(unsigned, lo), __builtin_bit_cast(unsigned, hi));
+    }
+}
+// Two of a 16-byte load's four words as the operand of one MFMA.
+template <int DT, int CT> __device__ __forceinline__ uint4 widen8(unsigned a, unsigned b) {
+    const uint2 lo = widen<DT, CT>(a), hi = widen<DT, CT>(b);
+    return make_uint4(lo.x, lo.y, hi.x, hi.y);
+}
+// ... between the surrounding fences: the conversions of a chunk are not all done ahead, where their results would fill the registers.
+template <int DT, int CT> __device__ __forceinline__ uint4 widen_here(unsigned a, unsigned b) {
+    asm volatile("" : "+v"(a), "+v"(b));
+    return widen8<DT, CT>(a, b);
+}
+template <int DT> __device__ __forceinline__ unsigned pack2(float a, float b) {
+    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    if constexpr (DT == DT_F16) {
+        const h2 v = {(_Float16)a, (_Float16)b};
+        return __builtin_bit_cast(unsigned, v);
+    } else {
+        const b2 v = {(__bf16)a, (__bf16)b};
+        return __builtin_bit_cast(unsigned, v);
+    }
+}
+__device__ __forceinline__ float half_max(float x) {      // over the two half-waves
+    const auto both = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+    const unsigned lo = both[0], hi = both[1];
+    return __builtin_fmaxf(__builtin_bit_cast(float, lo), __builtin_bit_cast(float, hi));
+}
+
+// log2 of the largest weight of a row
+template <int DT> __device__ __forceinline__ float weight_bits() { return DT == DT_F16 ? 14.f : 0.f; }
+
+// Partial results of a slice: a tile's accumulators, then its lanes' sums and references.
+template <int DH> constexpr int cache_partial_bytes() { return DH / 32 * 4096 + 512; }
+
+constexpr int kCacheWaves = 4;
+
+template <int DT, int CT, int DH>
+__global__ void __launch_bounds__(kCacheWaves * 64, 2) cache_rows_kernel(const CacheAttnParams p) {
+    constexpr int KG = kCacheWaves, DB = DH / 32, KL = DH / 32;      // 16-byte loads per lane of a 32-key chunk: KL of the keys, DB of the values
+    constexpr int MERGE = cache_partial_bytes<DH>();
+    __shared__ __attribute__((aligned(1024))) char smem[KG * MERGE];
+    const int lane = threadIdx.x & 63, l31 = lane & 31, g = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int tile = (int)blockIdx.x, slice = (int)blockIdx.y;
+    const int bh = (int)fastdiv((unsigned)tile, p.div_tiles_magic, p.div_tiles_shift);
+    const int rt = tile - bh * p.tiles;
+    const int b = (int)fastdiv((unsigned)bh, p.div_h_magic, p.div_h_shift);
+    const int h = bh - b * p.c.heads;
+    const int bt = 1 << p.c.shift;
+
+    const long long cap = (long long)p.c.cols << p.c.shift;          // < 2^31: the host checks
+    int len = p.lens[b], cnt = p.count ? p.count[b] : p.T;
+    len = len < 0 ? 0 : (len > (int)cap ? (int)cap : len);
+    cnt = cnt < 0 ? 0 : (cnt > p.T ? p.T : cnt);
+    const int row0 = rt * 32;
+    const int rows = cnt * p.G - row0;
+    if (rows <= 0) return;
+    // keys the rows of this tile see: up to the query's own position
+    const int t_lane = (int)fastdiv((unsigned)(row0 + l31), p.div_g_magic, p.div_g_shift);
+    const int g_lane = row0 + l31 - t_lane * p.G;
+    const bool live = l31 < rows;
+    const long long lim64 = (long long)len - cnt + t_lane + 1;
+    const int lim = live ? (int)(lim64 < 0 ? 0 : lim64) : 0;
+    const int t_first = (int)fastdiv((unsigned)row0, p.div_g_magic, p.div_g_shift);
+    const int r_last = rows < 32 ? rows - 1 : 31;
+    const int t_last = (int)fastdiv((unsigned)(row0 + r_last), p.div_g_magic, p.div_g_shift);
+    const long long kmax64 = (long long)len - cnt + t_last + 1, kmin64 = (long long)len - cnt + t_first + 1;
+    const int kmax = (int)(kmax64 < 0 ? 0 : kmax64), kmin = (int)(kmin64 < 0 ? 0 : kmin64);
+    const int nch = (kmax + 31) >> 5;
+    // this slice's chunks: at least two per wave
+    int per = (nch + p.slices - 1) / p.slices;
+    per = (per + KG - 1) / KG * KG;
+    per = per < 2 * KG ? 2 * KG : per;
+    const int active = nch > per ? (nch + per - 1) / per : 1;
+    if (slice >= active) return;
+    const int c_end = (slice + 1) * per < nch ? (slice + 1) * per : nch;
+    const int c_first = slice * per + wave;
+    const int mine = c_end > c_first ? (c_end - c_first + KG - 1) / KG : 0;
+
+    uint4 qf[DH / 16];
+    {
+        const char* const q = (const char*)p.Q + 2 * (b * p.q_bs + t_lane * p.q_rs + (long long)(h * p.G + g_lane) * p.q_hs);
+#pragma unroll
+        for (int ks = 0; ks < DH / 16; ++ks)          // step 2*jj + s takes channels (2*jj + g)*16 + 8*s ..: the order of the keys' 16-byte loads
+            qf[ks] = live ? *(const uint4*)(q + (((ks & ~1) + g) * 16 + (ks & 1) * 8) * 2) : make_uint4(0, 0, 0, 0);
+    }
+    f32x16 acc[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[db][r] = 0.f;
+    float m_run = -__FLT_MAX__, l_run = 0.f;
+
+    const int krow = 16 * ((l31 >> 2) & 1) + 4 * (l31 >> 3) + (l31 & 3);      // this lane's key of a chunk
+    const int* const table = p.c.table + (long long)b * p.c.cols;
+    // Block ids of this wave's next 32 chunks, one granule of 16 tokens per lane
+    auto fetch_ids = [&](int i0) __attribute__((always_inline)) -> int {
+        const long long gran = 2ll * (c_first + (i0 + (lane >> 1)) * KG) + (lane & 1);
+        const long long at = gran << 4 >> p.c.shift;
+        return i0 + (lane >> 1) < mine && (gran << 4) < len ? table[at < p.c.cols ? at : p.c.cols - 1] : -1;
+    };
+    int ids = fetch_ids(0), ids_next = 0;
+
+    struct Chunk {
+        u32x4 k[KL], v[DB];
+        float ks, vs;
+        int bad;                    // this half-wave's granule has no block
+    };
+    auto load = [&](int i, Chunk& c) __attribute__((always_inline)) {
+        const int at = (i & 31) * 2;
+        const int id0 = __builtin_amdgcn_readlane(ids, at), id1 = __builtin_amdgcn_readlane(ids, at + 1);
+        const bool ok0 = id0 >= 0 && id0 < p.c.blocks, ok1 = id1 >= 0 && id1 < p.c.blocks;
+        const long long bh0 = (long long)(ok0 ? id0 : 0) * p.c.heads + h, bh1 = (long long)(ok1 ? id1 : 0) * p.c.heads + h;
+        const int tok0 = (c_first + i * KG) * 32 & (bt - 1), tok1 = ((c_first + i * KG) * 32 + 16) & (bt - 1);      // in their blocks
+        const long long k0 = ((bh0 << p.c.shift) + tok0) * DH, k1 = ((bh1 << p.c.shift) + tok1) * DH - 16 * DH;
+        const char* const kp = p.c.k + ((l31 & 4) ? k1 : k0) + krow * DH + g * 16;
+#pragma unroll
+        for (int jj = 0; jj < KL; ++jj) c.k[jj] = *(const u32x4*)(kp + jj * 32);
+        const long long v0 = ((bh0 * DH) << p.c.shift) + tok0, v1 = ((bh1 * DH) << p.c.shift) + tok1;
+        const char* const vp = p.c.v + (g ? v1 : v0) + (l31 << p.c.shift);
+#pragma unroll
+        for (int db = 0; db < DB; ++db) c.v[db] = *(const u32x4*)(vp + ((db * 32) << p.c.shift));
+        c.ks = p.c.ks[g ? bh1 : bh0];
+        c.vs = p.c.vs[g ? bh1 : bh0];
+        c.bad = !(g ? ok1 : ok0);
+    };
+    auto step = [&](int i, Chunk& c) __attribute__((always_inline)) {
+        const int base = (c_first + i * KG) * 32;
+        f32x16 s;
+#pragma unroll
+        for (int ks = 0; ks < DH / 16; ++ks) {
+            const u32x4 w = c.k[ks >> 1];
+            const uint4 kf = (ks & 1) ? widen_here<DT, CT>(w[2], w[3]) : widen_here<DT, CT>(w[0], w[1]);
+            const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            s = InTraits<DT>::mfma(kf, qf[ks], ks == 0 ? zero : s);
+            TIR_FENCE();                      // the next operand is widened under this product, and not earlier: its registers are short
+        }
+        const float vs = __builtin_fmaxf(c.vs, 0x1p-100f);
+        const float mul = p.scale_log2e * c.ks, lvs = __builtin_amdgcn_logf(vs);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = __builtin_fmaf(s[r], mul, lvs);
+        const bool ragged = base + 32 > kmin || __builtin_amdgcn_ballot_w64(c.bad) != 0;
+        if (ragged) {
+            const int n = c.bad ? 0 : lim - base - 16 * g;      // keys of the lane's sixteen that its row sees
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = r < n ? s[r] : -__builtin_inff();
+            // what lies behind the sequence is not a value: e4m3 bytes there may be NaN, and NaN times a weight of zero is NaN
+            if constexpr (CT == CT_E4M3) {
+                const int nv = c.bad ? 0 : len - base - 16 * g;
+                u32x4 keep;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int left = nv - 4 * e;
+                    keep[e] = left >= 4 ? ~0u : (left <= 0 ? 0u : (1u << (8 * left)) - 1u);
+                }
+#pragma unroll
+                for (int db = 0; db < DB; ++db) c.v[db] = c.v[db] & keep;
+            }
+        }
+        float mx = s[0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) mx = __builtin_fmaxf(mx, s[r]);
+        mx = __builtin_fmaxf(half_max(mx), -__FLT_MAX__);
+        if (__builtin_amdgcn_ballot_w64(mx > m_run) != 0) {
+            const float m_new = __builtin_fmaxf(m_run, mx);
+            const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+            m_run = m_new;
+            l_run *= alpha;
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[db][r] *= alpha;
+        }
+        const float ref = m_run - weight_bits<DT>();
+        float sum[2] = {0.f, 0.f};
+        unsigned pw[8];
+#pragma unroll
+        for (int r = 0; r < 16; r += 2) {
+            float w[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                w[e] = __builtin_amdgcn_exp2f(s[r + e] - ref);
+                sum[e] += w[e];
+            }
+            pw[r / 2] = pack2<DT>(w[0], w[1]);
+        }
+        l_run += (sum[0] + sum[1]) * __builtin_amdgcn_rcpf(vs);
+#pragma unroll
+        for (int ss = 0; ss < 2; ++ss) {
+            const uint4 pf = make_uint4(pw[4 * ss], pw[4 * ss + 1], pw[4 * ss + 2], pw[4 * ss + 3]);
+#pragma unroll
+            for (int db = 0; db < DB; ++db) {
+                acc[db] = InTraits<DT>::mfma(widen_here<DT, CT>(c.v[db][2 * ss], c.v[db][2 * ss + 1]), pf, acc[db]);
+                TIR_FENCE();
+            }
+        }
+    };
+    // chunk i + 1 is on its way while chunk i is worked on; the ids of the next 32 chunks likewise
+    Chunk even, odd;
+    if (mine > 0) load(0, even);
+    for (int i = 0; i < mine; i += 2) {
+        if ((i & 31) == 0) ids_next = fetch_ids(i + 32);
+        if (i + 1 < mine) load(i + 1, odd);
+        step(i, even);
+        if (((i + 2) & 31) == 0) ids = ids_next;
+        if (i + 2 < mine) load(i + 2, even);
+        if (i + 1 < mine) step(i + 1, odd);
+    }
+
+    // ------------------------------------------------------------ the waves' results, relative to the largest reference
+    l_run += __shfl_xor(l_run, 32);
+    {
+        f32x4* const o = (f32x4*)(smem + wave * MERGE);
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4) {
+                f32x4 v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = acc[db][4 * q4 + e];
+                o[(db * 4 + q4) * 64 + lane] = v;
+            }
+        float* const t = (float*)(smem + wave * MERGE + DB * 4096);
+        t[lane] = l_run;
+        t[64 + lane] = m_run;
+    }
+    __syncthreads();
+    float top = -__FLT_MAX__, f[KG], l = 0.f;
+#pragma unroll
+    for (int k = 0; k < KG; ++k) {
+        f[k] = ((const float*)(smem + k * MERGE + DB * 4096))[64 + lane];
+        top = __builtin_fmaxf(top, f[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < KG; ++k) {
+        f[k] = __builtin_amdgcn_exp2f(f[k] - top);
+        l += f[k] * ((const float*)(smem + k * MERGE + DB * 4096))[lane];
+    }
+    constexpr int NG = DB * 4 / KG;                      // groups of four channels this wave finishes
+    static_assert(NG * KG == DB * 4, "");
+    f32x4 out[NG];
+#pragma unroll
+    for (int n = 0; n < NG; ++n) {
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < KG; ++k) v += f[k] * ((const f32x4*)(smem + k * MERGE))[(wave * NG + n) * 64 + lane];
+        out[n] = v;
+    }
+    if (active > 1) {
+        // Slices of a tile: as for the split reduction of a product, the partial results go through memory at system scope, the last to
+        // arrive adds them in slice order.
+        constexpr int kSystemScope = 17;
+        const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc((char*)p.ws + (long long)tile * p.slices * MERGE, 0, p.slices * MERGE, 0x00020000);
+#pragma unroll
+        for (int n = 0; n < NG; ++n)
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, out[n]), rw, ((wave * NG + n) * 64 + lane) * 16, slice * MERGE, kSystemScope);
+        if (wave == 0) {
+            __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, l), rw, DB * 4096 + lane * 4, slice * MERGE, kSystemScope);
+            __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, top), rw, DB * 4096 + 256 + lane * 4, slice * MERGE, kSystemScope);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        unsigned* const flag = (unsigned*)smem;
+        if (threadIdx.x == 0) *flag = __hip_atomic_fetch_add(p.ws_count + tile, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+        __syncthreads();
+        if (*flag != (unsigned)active - 1u) return;
+        if (threadIdx.x == 0) __hip_atomic_store(p.ws_count + tile, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+        top = -__FLT_MAX__;
+        for (int s = 0; s < active; ++s)
+            top = __builtin_fmaxf(top, __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rw, DB * 4096 + 256 + lane * 4, s * MERGE, kSystemScope)));
+        l = 0.f;
+#pragma unroll
+        for (int n = 0; n < NG; ++n) out[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < active; ++s) {
+            const float ms = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rw, DB * 4096 + 256 + lane * 4, s * MERGE, kSystemScope));
+            const float ls = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rw, DB * 4096 + lane * 4, s * MERGE, kSystemScope));
+            const float fs = __builtin_amdgcn_exp2f(ms - top);
+            l += fs * ls;
+#pragma unroll
+            for (int n = 0; n < NG; ++n)
+                out[n] += fs * __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, ((wave * NG + n) * 64 + lane) * 16, s * MERGE, kSystemScope));
+        }
+    }
+    if (!live) return;
+    const float inv = lim > 0 && l != 0.f ? 1.0f / l : 0.f;           // a row that sees no key is zero
+    const long long at = b * p.o_bs + t_lane * p.o_rs + (long long)(h * p.G + g_lane) * p.o_hs;
+#pragma unroll
+    for (int n = 0; n < NG; ++n) {
+        const int grp = wave * NG + n, ch = grp / 4 * 32 + grp % 4 * 8 + 4 * g;
+        const f32x4 v = out[n] * inv;
+        if (p.out32) *(f32x4*)((float*)p.O + at + ch) = v;
+        else *(uint2*)((unsigned short*)p.O + at + ch) = make_uint2(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]));
+    }
+}
+
+}  // namespace tir

@@ -1,0 +1,166 @@
+// Entry points of the paged cache and of attention over it: argument checks, choice of kernel, launch.
+#include <stdint.h>
+
+#include "tir_host.h"
+#include "tir_launch.h"
+#include "tir_cache.h"
+
+namespace tir {
+
+static const int64_t kMax31 = 2147483647LL;
+
+template <int DT, int CT, int DH> static hipError_t launch_append_as(const AppendParams& p, int64_t batch, hipStream_t stream) {
+    return launch_kernel(&cache_append_kernel<DT, CT, DH>, dim3((unsigned)(batch * p.touched * p.c.heads), 2), dim3(kAppendThreads), stream, p);
+}
+hipError_t launch_append(const AppendParams& p, int dt, int ct, int d, int64_t batch, hipStream_t stream) {
+#define TIR_APPEND(DT, CT, DH) if (dt == DT && ct == CT && d == DH) return launch_append_as<DT, CT, DH>(p, batch, stream);
+    TIR_APPEND(DT_F16, CT_I8, 64) TIR_APPEND(DT_F16, CT_I8, 128) TIR_APPEND(DT_F16, CT_E4M3, 64) TIR_APPEND(DT_F16, CT_E4M3, 128)
+    TIR_APPEND(DT_BF16, CT_I8, 64) TIR_APPEND(DT_BF16, CT_I8, 128) TIR_APPEND(DT_BF16, CT_E4M3, 64) TIR_APPEND(DT_BF16, CT_E4M3, 128)
+#undef TIR_APPEND
+    return hipErrorInvalidValue;
+}
+
+template <int DT, int CT, int DH> static hipError_t launch_cache_as(const CacheAttnParams& p, hipStream_t stream) {
+    return launch_kernel(&cache_rows_kernel<DT, CT, DH>, dim3((unsigned)(p.batch * p.c.heads * p.tiles), (unsigned)p.slices), dim3(kCacheWaves * 64), stream, p);
+}
+hipError_t launch_cache_attention(const CacheAttnParams& p, int dt, int ct, int d, hipStream_t stream) {
+#define TIR_CACHE(DT, CT, DH) if (dt == DT && ct == CT && d == DH) return launch_cache_as<DT, CT, DH>(p, stream);
+    TIR_CACHE(DT_F16, CT_I8, 64) TIR_CACHE(DT_F16, CT_I8, 128) TIR_CACHE(DT_F16, CT_E4M3, 64) TIR_CACHE(DT_F16, CT_E4M3, 128)
+    TIR_CACHE(DT_BF16, CT_I8, 64) TIR_CACHE(DT_BF16, CT_I8, 128) TIR_CACHE(DT_BF16, CT_E4M3, 64) TIR_CACHE(DT_BF16, CT_E4M3, 128)
+#undef TIR_CACHE
+    return hipErrorInvalidValue;
+}
+
+static tir_status check_cache(const char* who, const tir_kv_cache* c, int64_t batch, CacheView* out) {
+    if (!c) return host_error(TIR_ERR_INVALID_ARG, "%s: cache is null", who);
+    if (c->dtype != TIR_I8 && c->dtype != TIR_E4M3) return host_error(TIR_ERR_UNSUPPORTED, "%s: cache dtype %d (I8 and E4M3 are compiled)", who, (int)c->dtype);
+    if (c->d != 64 && c->d != 128) return host_error(TIR_ERR_UNSUPPORTED, "%s: head dimension %lld (64 and 128 are compiled)", who, (long long)c->d);
+    int shift = 0;
+    for (int s = 4; s <= 7; ++s)
+        if (c->block_tokens == (1 << s)) shift = s;
+    if (!shift) return host_error(TIR_ERR_UNSUPPORTED, "%s: blocks of %lld tokens (16, 32, 64 and 128 are compiled)", who, (long long)c->block_tokens);
+    if (c->blocks < 1 || c->heads < 1 || c->columns < 1) return host_error(TIR_ERR_INVALID_ARG, "%s: cache of %lld blocks, %lld heads and %lld columns: at least one of each is needed", who, (long long)c->blocks, (long long)c->heads, (long long)c->columns);
+    if (c->blocks > kMax31 || c->heads > 65535 || c->columns > (kMax31 >> shift)) return host_error(TIR_ERR_UNSUPPORTED, "%s: cache extent beyond 2^31-1 (columns * block_tokens included) or more than 65535 heads", who);
+    if (!c->k || !c->v || !c->k_scale || !c->v_scale || !c->table) return host_error(TIR_ERR_INVALID_ARG, "%s: a pointer of the cache is null", who);
+    if (!host_aligned(c->k, 16) || !host_aligned(c->v, 16)) return host_error(TIR_ERR_ALIGNMENT, "%s: the cache's k and v must be 16-byte aligned", who);
+    if (!host_aligned(c->k_scale, 4) || !host_aligned(c->v_scale, 4) || !host_aligned(c->table, 4)) return host_error(TIR_ERR_ALIGNMENT, "%s: the cache's scales and table must be 4-byte aligned", who);
+    (void)batch;
+    out->k = (char*)c->k;
+    out->v = (char*)c->v;
+    out->ks = c->k_scale;
+    out->vs = c->v_scale;
+    out->table = c->table;
+    out->blocks = (int)c->blocks;
+    out->heads = (int)c->heads;
+    out->cols = (int)c->columns;
+    out->shift = shift;
+    return TIR_OK;
+}
+
+// Strides of rows that are read or written 16 bytes at a time.  `last`: largest index along each; the offsets have to fit 62 bits.
+static tir_status check_strides(const char* who, const char* what, int64_t bs, int64_t rs, int64_t hs) {
+    if (bs < 0 || rs < 0 || hs < 0) return host_error(TIR_ERR_INVALID_ARG, "%s: negative stride of %s", who, what);
+    if ((bs | rs | hs) & 7) return host_error(TIR_ERR_ALIGNMENT, "%s: the strides of %s must be multiples of 8 elements", who, what);
+    if (bs > (1ll << 40) || rs > (1ll << 40) || hs > (1ll << 40)) return host_error(TIR_ERR_UNSUPPORTED, "%s: stride of %s beyond 2^40", who, what);
+    return TIR_OK;
+}
+
+}  // namespace tir
+
+using namespace tir;
+
+extern "C" {
+
+tir_status tir_cache_append(const tir_kv_cache* cache, const void* K, const void* V, const int32_t* start,
+                            const int32_t* count, int64_t batch, int64_t T, int64_t k_bs, int64_t k_rs, int64_t k_hs,
+                            int64_t v_bs, int64_t v_rs, int64_t v_hs, tir_dtype in, tir_stream stream) {
+    const char* const who = "cache append";
+    if ((int)in < 0 || (int)in > TIR_E4M3) return host_error(TIR_ERR_INVALID_ARG, "unknown dtype code (in=%d)", (int)in);
+    if (in != TIR_F16 && in != TIR_BF16) return host_error(TIR_ERR_UNSUPPORTED, "%s: unsupported input dtype %d", who, (int)in);
+    if (batch < 0 || T < 0) return host_error(TIR_ERR_INVALID_ARG, "negative extent (batch=%lld T=%lld)", (long long)batch, (long long)T);
+    AppendParams p = {};
+    tir_status st = check_cache(who, cache, batch, &p.c);
+    if (st == TIR_OK) st = check_strides(who, "K", k_bs, k_rs, k_hs);
+    if (st == TIR_OK) st = check_strides(who, "V", v_bs, v_rs, v_hs);
+    if (st != TIR_OK) return st;
+    if (batch == 0 || T == 0) return TIR_OK;
+    if (!K || !V || !start) return host_error(TIR_ERR_INVALID_ARG, "%s: K, V or start is null", who);
+    if (!host_aligned(K, 16) || !host_aligned(V, 16)) return host_error(TIR_ERR_ALIGNMENT, "%s: K and V must be 16-byte aligned", who);
+    if (!host_aligned(start, 4) || !host_aligned(count, 4)) return host_error(TIR_ERR_ALIGNMENT, "%s: start and count must be 4-byte aligned", who);
+    if (T > kMax31 - 128 || batch > kMax31) return host_error(TIR_ERR_UNSUPPORTED, "extent beyond 2^31-1");
+    int64_t touched = (T + (1 << p.c.shift) - 2) / (1 << p.c.shift) + 1;      // T tokens from any position on
+    if (touched > p.c.cols) touched = p.c.cols;
+    if (batch * touched > kMax31 / p.c.heads) return host_error(TIR_ERR_UNSUPPORTED, "%s: too many blocks in one call", who);
+    p.K = K; p.V = V;
+    p.k_bs = k_bs; p.k_rs = k_rs; p.k_hs = k_hs;
+    p.v_bs = v_bs; p.v_rs = v_rs; p.v_hs = v_hs;
+    p.start = start; p.count = count;
+    p.T = (int)T;
+    p.touched = (int)touched;
+    const FastDiv dh = make_fastdiv((unsigned)p.c.heads), dt = make_fastdiv((unsigned)touched);
+    p.div_h_magic = dh.magic; p.div_h_shift = dh.shift;
+    p.div_t_magic = dt.magic; p.div_t_shift = dt.shift;
+    const hipError_t e = launch_append(p, (int)in, cache->dtype == TIR_I8 ? CT_I8 : CT_E4M3, (int)cache->d, batch, (hipStream_t)stream);
+    if (e != hipSuccess) return host_error(TIR_ERR_LAUNCH, "%s: launch failed: %s", who, hipGetErrorString(e));
+    return TIR_OK;
+}
+
+tir_status tir_cache_attention(const void* Q, const tir_kv_cache* cache, void* O, const int32_t* lens,
+                               const int32_t* count, int64_t batch, int64_t T, int64_t Hq, int64_t q_bs, int64_t q_rs,
+                               int64_t q_hs, int64_t o_bs, int64_t o_rs, int64_t o_hs, float scale, tir_dtype in,
+                               tir_dtype out, tir_stream stream) {
+    const char* const who = "cache attention";
+    if ((int)in < 0 || (int)in > TIR_E4M3 || (int)out < 0 || (int)out > TIR_E4M3) return host_error(TIR_ERR_INVALID_ARG, "unknown dtype code (in=%d out=%d)", (int)in, (int)out);
+    if (!((in == TIR_F16 || in == TIR_BF16) && (out == in || out == TIR_F32))) return host_error(TIR_ERR_UNSUPPORTED, "%s: unsupported (in, out) dtype pair (%d, %d)", who, (int)in, (int)out);
+    if (batch < 0 || T < 0 || Hq < 0) return host_error(TIR_ERR_INVALID_ARG, "negative extent (batch=%lld T=%lld Hq=%lld)", (long long)batch, (long long)T, (long long)Hq);
+    CacheAttnParams p = {};
+    tir_status st = check_cache(who, cache, batch, &p.c);
+    if (st == TIR_OK) st = check_strides(who, "Q", q_bs, q_rs, q_hs);
+    if (st == TIR_OK) st = check_strides(who, "O", o_bs, o_rs, o_hs);
+    if (st != TIR_OK) return st;
+    if (!(scale == scale) || scale > 3.0e38f || scale < -3.0e38f) return host_error(TIR_ERR_INVALID_ARG, "%s: scale must be finite", who);
+    if (Hq % p.c.heads) return host_error(TIR_ERR_INVALID_ARG, "%s: %d key heads do not divide %lld query heads", who, p.c.heads, (long long)Hq);
+    if (batch == 0 || T == 0 || Hq == 0) return TIR_OK;
+    if (!Q || !O || !lens) return host_error(TIR_ERR_INVALID_ARG, "%s: Q, O or lens is null", who);
+    if (!host_aligned(Q, 16) || !host_aligned(O, 16)) return host_error(TIR_ERR_ALIGNMENT, "%s: Q and O must be 16-byte aligned", who);
+    if (!host_aligned(lens, 4) || !host_aligned(count, 4)) return host_error(TIR_ERR_ALIGNMENT, "%s: lens and count must be 4-byte aligned", who);
+    if ((batch > 1 && o_bs == 0) || (T > 1 && o_rs == 0) || (Hq > 1 && o_hs == 0)) return host_error(TIR_ERR_INVALID_ARG, "%s: a stride of O is zero: its rows overlap", who);
+    if (T > kMax31 || Hq > kMax31 || T > (kMax31 - 64) / (Hq / p.c.heads)) return host_error(TIR_ERR_UNSUPPORTED, "extent beyond 2^31-1");
+    p.G = (int)(Hq / p.c.heads);
+    p.T = (int)T;
+    const int64_t tiles = (T * p.G + 31) / 32;
+    if (batch > kMax31 / p.c.heads || batch * p.c.heads > kMax31 / tiles) return host_error(TIR_ERR_UNSUPPORTED, "%s: too many tiles of queries", who);
+    p.batch = (int)batch;
+    p.tiles = (int)tiles;
+    p.Q = Q; p.O = O;
+    p.q_bs = q_bs; p.q_rs = q_rs; p.q_hs = q_hs;
+    p.o_bs = o_bs; p.o_rs = o_rs; p.o_hs = o_hs;
+    p.lens = lens; p.count = count;
+    p.out32 = out == TIR_F32;
+    p.scale_log2e = scale * 1.44269504088896340736f;
+    const FastDiv dg = make_fastdiv((unsigned)p.G), dh = make_fastdiv((unsigned)p.c.heads), dt = make_fastdiv((unsigned)tiles);
+    p.div_g_magic = dg.magic; p.div_g_shift = dg.shift;
+    p.div_h_magic = dh.magic; p.div_h_shift = dh.shift;
+    p.div_tiles_magic = dt.magic; p.div_tiles_shift = dt.shift;
+    p.slices = 1;
+    const int64_t groups = batch * p.c.heads * tiles;
+    const StreamWorkspace ws = stream_workspace((hipStream_t)stream);
+    if (ws.partial && groups <= ws.counters && groups < 512) {
+        const int64_t part = cache->d == 64 ? cache_partial_bytes<64>() : cache_partial_bytes<128>();
+        int64_t slices = (512 + groups - 1) / groups;
+        const int64_t chunks = (((int64_t)p.c.cols << p.c.shift) + 31) / 32;
+        if (slices > (chunks + 7) / 8) slices = (chunks + 7) / 8;
+        if (slices > 64) slices = 64;
+        if (slices > ws.bytes / (groups * part)) slices = ws.bytes / (groups * part);
+        if (slices > 1) {
+            p.slices = (int)slices;
+            p.ws = ws.partial;
+            p.ws_count = ws.count;
+        }
+    }
+    const hipError_t e = launch_cache_attention(p, (int)in, cache->dtype == TIR_I8 ? CT_I8 : CT_E4M3, (int)cache->d, (hipStream_t)stream);
+    if (e != hipSuccess) return host_error(TIR_ERR_LAUNCH, "%s: launch failed: %s", who, hipGetErrorString(e));
+    return TIR_OK;
+}
+
+}  // extern "C"
