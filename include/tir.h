@@ -242,6 +242,22 @@ tir_status tir_cache_attention(const void* Q, const tir_kv_cache* cache, void* O
                                int64_t q_hs, int64_t o_bs, int64_t o_rs, int64_t o_hs, float scale, tir_dtype in,
                                tir_dtype out, tir_stream stream);
 
+/*
+ * Attention over the states of another sequence, such as an encoder's: sequence b has M queries and lens[b] keys (int32 [batch] on the device; values outside
+ * [0, N] count as the nearest inside; NULL: N each), every query sees all of them:
+ *     O[b,i,hq] = sum_j p_j * V[b,j,hk],  p = softmax over j < lens[b] of scale * (Q[b,i,hq] . K[b,j,hk]),  hk = hq / (Hq / Hkv)
+ * Q[b*q_bs + i*q_rs + hq*q_hs + c], c < d, and likewise K, V (by hk) and O; Hkv must divide Hq, d is 64 or 128.  Keys and values from lens[b] on are not used, whatever they
+ * hold.  A sequence without keys gives zeros.  lse: fp32 [batch][Hq][M], dense, log(sum_j exp(scale * Q.K)), -infinity without keys, which the backward pass
+ * needs; NULL where it is not wanted.  in = F16 or BF16; out = the same type or F32.  Arithmetic and accuracy as tir_attention; lse to 1e-5 + 2^-22 * max|scale * Q.K|.
+ * With a workspace registered for `stream` few queries over many keys are shared among workgroups, whose results are added in a fixed order.
+ * Pointers 16-byte aligned, all strides multiples of 8 elements, row strides at most 2^23; those of O must keep its rows apart, those of the inputs may be 0.  batch, M or Hq = 0 is a no-op.
+ */
+tir_status tir_cross_attention(const void* Q, const void* K, const void* V, void* O, float* lse, const int32_t* lens,
+                               int64_t batch, int64_t M, int64_t N, int64_t Hq, int64_t Hkv, int64_t d, int64_t q_bs,
+                               int64_t q_rs, int64_t q_hs, int64_t k_bs, int64_t k_rs, int64_t k_hs, int64_t v_bs,
+                               int64_t v_rs, int64_t v_hs, int64_t o_bs, int64_t o_rs, int64_t o_hs, float scale,
+                               tir_dtype in, tir_dtype out, tir_stream stream);
+
 /* Message for the calling thread's last failed call ("" if none).  Never NULL; valid until the
  * thread's next failing call. */
 const char* tir_last_error(void);

@@ -29,6 +29,20 @@ struct AttnParams {
     int store_nt;            // the output is not read again soon: non-temporal stores (see TIR_STORE_AUX_STREAM)
 };
 
+// Attention over the states of another sequence: row r of a (sequence, key head) is position r / G of its query head r % G, so that the query heads that
+// share a key head share its copies; strides throughout, lengths per sequence, and few rows over many keys shared among workgroups.
+struct CrossParams : AttnParams {      // M: positions * G, N: largest number of keys, batch: sequences * key heads
+    long long q_bs, q_rs, q_hs, k_bs, k_rs, k_hs, v_bs, v_rs, v_hs, o_bs, o_rs, o_hs;      // in elements
+    const int* lens;         // keys of each sequence; null: N each
+    float* lse;              // [sequences][query heads][positions], or null
+    int heads, G, positions;      // key heads, query heads per key head, rows of a query head
+    int slices;              // workgroups that share a tile's keys
+    void* ws;                // slices > 1: partial results [tile][slice][kernel's MERGE * QW]
+    unsigned* ws_count;      // ... and arrival counters [tile], zero between launches
+    unsigned div_h_magic, div_g_magic;      // / heads, / G
+    int div_h_shift, div_g_shift;
+};
+
 template <int DT> struct PackP;
 template <> struct PackP<DT_F16> {
     static __device__ __forceinline__ unsigned two(float a, float b) {
@@ -63,8 +77,12 @@ template <> struct PackP<DT_BF16> {
 // FORM: the loop described above, plain or with non-temporal copies, or a chunk's phases in sequence.  The latter holds one chunk's scores instead of two: 109 to 112
 // registers instead of 161 to 163 at d = 64, four workgroups per CU instead of three.
 enum : int { ATTN_PIPED = 0, ATTN_PIPED_STREAM = 1, ATTN_SEQUENTIAL = 2 };
-template <int DT, int OUT, int DH, int QW, int KG, int KB, int FORM>
-__global__ void __launch_bounds__(QW * KG * 64, 2) attention_kernel(const AttnParams p) {
+//
+// P: AttnParams (dense heads) or CrossParams.
+template <int DT, int OUT, int DH, int QW, int KG, int KB, int FORM, class P = AttnParams>
+__global__ void __launch_bounds__(QW * KG * 64, 2) attention_kernel(const P p) {
+    constexpr bool CROSS = std::is_same<P, CrossParams>::value;
+    constexpr bool SPLIT = CROSS && KG > 1;      // the form for few rows: its tiles' keys may be shared among workgroups
     typedef OutTraits<OUT> OT;
     typedef typename OT::type out_t;
     constexpr int OS = (int)sizeof(out_t);
@@ -107,14 +125,69 @@ __global__ void __launch_bounds__(QW * KG * 64, 2) attention_kernel(const AttnPa
     const int tm = bid - (int)b * p.tiles_m;
     const int m0 = tm * TQ;
     const int rows_q = p.M - m0 < TQ ? p.M - m0 : TQ;
-    const int nchunk = (p.N + KB - 1) / KB;
+    // this tile's sequence and key head, its number of keys
+    const int seq = [&]() { if constexpr (CROSS) return (int)fastdiv((unsigned)b, p.div_h_magic, p.div_h_shift); else return 0; }();
+    const int head = [&]() { if constexpr (CROSS) return (int)b - seq * p.heads; else return 0; }();
+    const int keys_n = [&]() {
+        if constexpr (CROSS) {
+            const int n = p.lens ? p.lens[seq] : p.N;
+            return n < 0 ? 0 : (n > p.N ? p.N : n);
+        } else return p.N;
+    }();
+    // of row `row` of the tile, in elements
+    auto row_at = [&](int row, long long bs, long long rs, long long hs) __attribute__((always_inline)) -> long long {
+        if constexpr (CROSS) {
+            const int m = (int)fastdiv((unsigned)(m0 + row), p.div_g_magic, p.div_g_shift);
+            return seq * bs + m * rs + (long long)(head * p.G + (m0 + row - m * p.G)) * hs;
+        }
+        return 0;
+    };
+    auto lse_at = [&](int row) __attribute__((always_inline)) -> long long {
+        if constexpr (CROSS) {
+            const int m = (int)fastdiv((unsigned)(m0 + row), p.div_g_magic, p.div_g_shift);
+            return ((long long)seq * p.heads * p.G + head * p.G + (m0 + row - m * p.G)) * p.positions + m;
+        }
+        return 0;
+    };
+    if constexpr (CROSS) {
+        if (keys_n == 0) {            // nothing to see: zeros
+            if (SPLIT && blockIdx.y > 0) return;
+            constexpr int ORC = DH * OS / 16;
+            for (int q = (int)threadIdx.x; q < rows_q * ORC; q += GT * KG)
+                *(uint4*)((out_t*)p.O + row_at(q / ORC, p.o_bs, p.o_rs, p.o_hs) + q % ORC * (16 / OS)) = make_uint4(0, 0, 0, 0);
+            if (p.lse)
+                for (int r = (int)threadIdx.x; r < rows_q; r += GT * KG) p.lse[lse_at(r)] = -__builtin_inff();
+            return;
+        }
+    }
+    const int nchunk_all = (keys_n + KB - 1) / KB;
+    // This workgroup's run of chunks, at least two per key group, and how many workgroups have one.
+    const int per = [&]() {
+        if constexpr (SPLIT) {
+            const int even = ((nchunk_all + p.slices - 1) / p.slices + KG - 1) / KG * KG;
+            return p.slices > 1 ? (even < 2 * KG ? 2 * KG : even) : nchunk_all;
+        } else return 0;
+    }();
+    const int slices = [&]() { if constexpr (SPLIT) return (nchunk_all + per - 1) / per; else return 1; }();
+    if constexpr (SPLIT) {
+        if ((int)blockIdx.y >= slices) return;
+    }
+    const int chunk0 = [&]() { if constexpr (SPLIT) return (int)blockIdx.y * per; else return 0; }();
+    const int nchunk = [&]() { if constexpr (SPLIT) return nchunk_all - chunk0 < per ? nchunk_all - chunk0 : per; else return nchunk_all; }();
     const int nmine = (nchunk - kgrp + KG - 1) / KG;             // this group's chunks (chunk i of it is i * KG + kgrp)
     const int nloop = (nchunk + KG - 1) / KG;                    // ... of the longest group: all take part in its barriers
 
     // ------------------------------------------------------------ copy stage
     // K-major tile: HALVES sub-tiles of [KB rows][128 B] so that the row swizzle of the GEMM kernels applies unchanged.
     unsigned k_off, v_off;                            // the lane's offsets of the first copy instruction; the others are scalars further on
-    {
+    // (bytes from one copy instruction's rows to the next one's, where rows are strided)
+    const int k_step = [&]() { if constexpr (CROSS) return KROWS * (int)p.k_rs * 2; else return 0; }();
+    const int v_step = [&]() { if constexpr (CROSS) return GT / VRC * (int)p.v_rs * 2; else return 0; }();
+    if constexpr (CROSS) {
+        const int row = tid >> 3, key = tid / VRC;
+        k_off = (unsigned)(row * (int)p.k_rs * 2 + (((tid & 7) ^ kmajor_swz<128>(row)) << 4));
+        v_off = (unsigned)(key * (int)p.v_rs * 2 + (((tid % VRC) * 16) ^ (((key / RPW) % NSEG) * 64)));
+    } else {
         const int row = tid >> 3;
         k_off = (unsigned)(row * ROW + (((tid & 7) ^ kmajor_swz<128>(row)) << 4));
         const int key = tid / VRC;
@@ -122,8 +195,8 @@ __global__ void __launch_bounds__(QW * KG * 64, 2) attention_kernel(const AttnPa
         static_assert((GT / VRC) % (RPW * NSEG) == 0, "the V swizzle repeats from one copy instruction to the next");
     }
     const char* Qb = (const char*)p.Q + ((b * p.M + m0) * (long long)ROW);
-    const char* Kb = (const char*)p.K + b * p.N * (long long)ROW;
-    const char* Vb = (const char*)p.V + b * p.N * (long long)ROW;
+    const char* Kb = [&]() { if constexpr (CROSS) return (const char*)p.K + 2 * (seq * p.k_bs + head * p.k_hs); else return (const char*)p.K + b * p.N * (long long)ROW; }();
+    const char* Vb = [&]() { if constexpr (CROSS) return (const char*)p.V + 2 * (seq * p.v_bs + head * p.v_hs); else return (const char*)p.V + b * p.N * (long long)ROW; }();
     // Non-temporal copies of the first two chunks for what one workgroup alone reads (one tile holds all queries of a head): 192 heads of
     // 128 x 128 x 64 from memory 7.05 -> 6.63 us, no change from the caches.
     const bool kv_once = p.tiles_m == 1;
@@ -131,22 +204,39 @@ __global__ void __launch_bounds__(QW * KG * 64, 2) attention_kernel(const AttnPa
     // addition per LDS read).
     auto copy_key = [&](const i32x4& rk, int st, int u, bool once) __attribute__((always_inline)) {
         char* const dst = ring + st * 2 * TILE + wave * 1024 + u / KPASS * (KB * 128) + u % KPASS * (GT * 16);
+        if constexpr (CROSS) {
+            const int at = u % KPASS * k_step + u / KPASS * 128;
+            if (once) load_to_lds_nt(rk, dst, k_off + at);
+            else load_to_lds_at(rk, dst, k_off, at);
+            return;
+        }
         const unsigned off = k_off + u % KPASS * (KROWS * ROW) + u / KPASS * 128;
         if (once) load_to_lds_nt(rk, dst, off);
         else load_to_lds(rk, dst, off);
     };
     auto copy_value = [&](const i32x4& rv, int st, int u, bool once) __attribute__((always_inline)) {
         char* const dst = ring + st * 2 * TILE + TILE + wave * 1024 + u * (GT * 16);
+        if constexpr (CROSS) {
+            if (once) load_to_lds_nt(rv, dst, v_off + u * v_step);
+            else load_to_lds_at(rv, dst, v_off, u * v_step);
+            return;
+        }
         if (once) load_to_lds_nt(rv, dst, v_off + u * (GT * 16));
         else load_to_lds(rv, dst, v_off + u * (GT * 16));
     };
+    const long long k_rs = [&]() { if constexpr (CROSS) return p.k_rs; else return 0ll; }();
+    const long long v_rs = [&]() { if constexpr (CROSS) return p.v_rs; else return 0ll; }();
     // Descriptor of chunk i of this group in K or V: rows past N lie outside it and read zeros; past the last chunk it is empty.
-    auto chunk_rsrc = [&](const char* base, int i) __attribute__((always_inline)) {
+    auto chunk_rsrc = [&](const char* base, int i, long long rs) __attribute__((always_inline)) {
+        if constexpr (CROSS) {
+            const int c = chunk0 + i * KG + kgrp, left = i * KG + kgrp < nchunk ? keys_n - c * KB : 0;
+            return make_rsrc(base + (long long)c * KB * rs * 2, left > 0 ? (left - 1) * rs * 2 + ROW : 0);
+        }
         const int c = i * KG + kgrp;
         return make_rsrc(base + (long long)c * TILE, (long long)(p.N - c * KB) * ROW);
     };
     auto copy_keys = [&](int i, int st) __attribute__((always_inline)) {
-        const i32x4 rk = chunk_rsrc(Kb, i);
+        const i32x4 rk = chunk_rsrc(Kb, i, k_rs);
         if (kv_once) {
 #pragma unroll
             for (int u = 0; u < COPIES; ++u) copy_key(rk, st, u, true);
@@ -156,7 +246,7 @@ __global__ void __launch_bounds__(QW * KG * 64, 2) attention_kernel(const AttnPa
         }
     };
     auto copy_values = [&](int i, int st) __attribute__((always_inline)) {
-        const i32x4 rv = chunk_rsrc(Vb, i);
+        const i32x4 rv = chunk_rsrc(Vb, i, v_rs);
         if (kv_once) {
 #pragma unroll
             for (int u = 0; u < COPIES; ++u) copy_value(rv, st, u, true);
@@ -173,7 +263,16 @@ __global__ void __launch_bounds__(QW * KG * 64, 2) attention_kernel(const AttnPa
     // (no non-temporal hint here, although nobody else reads them: a load takes 32 bytes of each of 32 rows, and lines that do not stay are
     // fetched again by the next one - 6.76 us instead of 6.20 for the same heads)
     uint4 qf[KSTEPS];
-    {
+    if constexpr (CROSS) {
+        const int row = wave * 32 + l31;
+        const char* const q = (const char*)p.Q + 2 * row_at(row, p.q_bs, p.q_rs, p.q_hs);
+#pragma unroll
+        for (int ks = 0; ks < KSTEPS; ++ks) qf[ks] = make_uint4(0, 0, 0, 0);
+        if (row < rows_q) {
+#pragma unroll
+            for (int ks = 0; ks < KSTEPS; ++ks) qf[ks] = *(const uint4*)(q + ks * 32 + g * 16);
+        }
+    } else {
         const __amdgpu_buffer_rsrc_t rq = __builtin_amdgcn_make_buffer_rsrc((void*)Qb, 0, rows_q * ROW, 0x00020000);
         typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 #pragma unroll
@@ -229,13 +328,13 @@ __global__ void __launch_bounds__(QW * KG * 64, 2) attention_kernel(const AttnPa
     const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     // keys past N (only in the last chunk) drop out of the softmax
     auto mask_chunk = [&](int i, f32x16 (&s)[JB]) __attribute__((always_inline)) {
-        const int c = i * KG + kgrp;
-        if ((c + 1) * KB > p.N) {
+        const int c = chunk0 + i * KG + kgrp;
+        if ((c + 1) * KB > keys_n) {
 #pragma unroll
             for (int jb = 0; jb < JB; ++jb)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    if (c * KB + jb * 32 + 8 * (r >> 2) + 4 * g + (r & 3) >= p.N) s[jb][r] = -__builtin_inff();
+                    if (c * KB + jb * 32 + 8 * (r >> 2) + 4 * g + (r & 3) >= keys_n) s[jb][r] = -__builtin_inff();
         }
     };
     // A row's largest scaled score in a chunk from the lane's partial maxima.
@@ -273,13 +372,13 @@ __global__ void __launch_bounds__(QW * KG * 64, 2) attention_kernel(const AttnPa
         if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(__builtin_fabsf(m_run) <= fused_upto)) != 0, 0)) {
 #pragma clang fp contract(off)
             // exponents in place of the scores; keys past N again, which a scale of zero would turn into NaN
-            const int c = i * KG + kgrp;
+            const int c = chunk0 + i * KG + kgrp;
 #pragma unroll
             for (int jb = 0; jb < JB; ++jb)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const float s = cur[jb][r] * sc;
-                    cur[jb][r] = c * KB + jb * 32 + 8 * (r >> 2) + 4 * g + (r & 3) >= p.N ? -__builtin_inff() : s - m_run;
+                    cur[jb][r] = c * KB + jb * 32 + 8 * (r >> 2) + 4 * g + (r & 3) >= keys_n ? -__builtin_inff() : s - m_run;
                 }
             mul = 1.f;
             base = 0.f;
@@ -287,7 +386,7 @@ __global__ void __launch_bounds__(QW * KG * 64, 2) attention_kernel(const AttnPa
         if constexpr (!LAST && !COPY) {
             if (i > 0) copy_values(i + 1, st ^ 1);
         }
-        const i32x4 rk = chunk_rsrc(Kb, i + 2), rv = chunk_rsrc(Vb, i + 1);
+        const i32x4 rk = chunk_rsrc(Kb, i + 2, k_rs), rv = chunk_rsrc(Vb, i + 1, v_rs);
         unsigned pw[JB * 8];                                         // P^T fragments: key block jb, k-step s at 8*jb + 4*s
         float lsum[2] = {0.f, 0.f};
         uint4 kf[LAK], vf[LAV];
@@ -446,6 +545,7 @@ __global__ void __launch_bounds__(QW * KG * 64, 2) attention_kernel(const AttnPa
                 top = __builtin_fmaxf(top, mk[k]);
             }
             const float own = __builtin_amdgcn_exp2f(mk[0] - top);             // (group 0 always has a chunk: top is finite)
+            if constexpr (CROSS) m_run = top;
             l_run *= own;
 #pragma unroll
             for (int db = 0; db < DB; ++db)
@@ -470,7 +570,66 @@ __global__ void __launch_bounds__(QW * KG * 64, 2) attention_kernel(const AttnPa
     }
 
     // ------------------------------------------------------------ normalise, stage through LDS, store rows
-    const float l_tot = l_run + __shfl_xor(l_run, 32);
+    float l_tot = l_run + __shfl_xor(l_run, 32);
+    if constexpr (SPLIT) {
+        if (slices > 1) {
+            // As for the split reduction of a product: the partial results go through memory at system scope, the slice that arrives last adds all of them in slice order.
+            typedef float f32x4 __attribute__((ext_vector_type(4)));
+            typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+            constexpr int kSystemScope = 17, PART = QW * MERGE;
+            const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc((char*)p.ws + (long long)bid * p.slices * PART, 0, p.slices * PART, 0x00020000);
+            const int at = wave * MERGE + lane * 16, at_l = wave * MERGE + DB * 4096 + lane * 4;
+            if (kgrp == 0) {
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+#pragma unroll
+                    for (int q4 = 0; q4 < 4; ++q4) {
+                        f32x4 v;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[e] = acc_o[db][4 * q4 + e];
+                        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), rw, at + (db * 4 + q4) * 1024, (int)blockIdx.y * PART, kSystemScope);
+                    }
+                __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, l_tot), rw, at_l, (int)blockIdx.y * PART, kSystemScope);
+                __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, m_run), rw, at_l + 256, (int)blockIdx.y * PART, kSystemScope);
+            }
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            unsigned* const flag = (unsigned*)smem;
+            if (threadIdx.x == 0) *flag = __hip_atomic_fetch_add(p.ws_count + bid, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+            __syncthreads();
+            const bool last = *flag == (unsigned)slices - 1u;
+            __syncthreads();                               // (the flag's place becomes the output tile's)
+            if (!last) return;
+            if (threadIdx.x == 0) __hip_atomic_store(p.ws_count + bid, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+            if (kgrp == 0) {
+                float top = -__FLT_MAX__;
+                for (int z = 0; z < slices; ++z)
+                    top = __builtin_fmaxf(top, __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rw, at_l + 256, z * PART, kSystemScope)));
+                m_run = top;
+                l_tot = 0.f;
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc_o[db][r] = 0.f;
+                for (int z = 0; z < slices; ++z) {
+                    const float f = __builtin_amdgcn_exp2f(__builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rw, at_l + 256, z * PART, kSystemScope)) - top);
+                    l_tot += f * __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rw, at_l, z * PART, kSystemScope));
+#pragma unroll
+                    for (int db = 0; db < DB; ++db)
+#pragma unroll
+                        for (int q4 = 0; q4 < 4; ++q4) {
+                            const f32x4 v = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, at + (db * 4 + q4) * 1024, z * PART, kSystemScope));
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc_o[db][4 * q4 + e] += f * v[e];
+                        }
+                }
+            }
+        }
+    }
+    if constexpr (CROSS) {
+        const int row = wave * 32 + l31;
+        if (p.lse && kgrp == 0 && g == 0 && row < rows_q) p.lse[lse_at(row)] = (m_run + __builtin_amdgcn_logf(l_tot)) * 0.69314718055994530942f;
+    }
     const float inv = 1.0f / l_tot;
     constexpr int ORB = DH * OS;                     // bytes of one output row
     char* const s_o = smem;                          // the K / V stages are free now
@@ -490,7 +649,15 @@ __global__ void __launch_bounds__(QW * KG * 64, 2) attention_kernel(const AttnPa
             else *(uint2*)dst = *(const uint2*)v;
         }
     __syncthreads();
-    {
+    if constexpr (CROSS) {
+        constexpr int ORC = ORB / 16;
+#pragma unroll
+        for (int i = 0; i < TQ * ORC / (GT * KG); ++i) {
+            const int q = (int)threadIdx.x + i * GT * KG;
+            const int row = q / ORC, pc = q % ORC;
+            if (row < rows_q) *(uint4*)((out_t*)p.O + row_at(row, p.o_bs, p.o_rs, p.o_hs) + pc * (16 / OS)) = *(const uint4*)(s_o + row * ORB + ((pc * 16) ^ ((row & 7) << 4)));
+        }
+    } else {
         char* Ob = (char*)p.O + (b * p.M + m0) * (long long)ORB;
         const __amdgpu_buffer_rsrc_t ro = __builtin_amdgcn_make_buffer_rsrc((void*)Ob, 0, rows_q * ORB, 0x00020000);
         constexpr int ORC = ORB / 16;                // 16-byte chunks per output row
@@ -513,5 +680,9 @@ AttnKernel attention_kernel_of(long long batch, long long M, long long N, int DH
 typedef hipError_t (*attn_launch_fn)(const AttnParams&, hipStream_t);
 // (dt, out, head dimension) -> launcher, or null when the combination is not compiled
 attn_launch_fn attention_launcher(int dt, int out, int dh);
+
+// The same for attention over another sequence's states.
+typedef hipError_t (*cross_launch_fn)(const CrossParams&, hipStream_t);
+cross_launch_fn cross_launcher(int dt, int out, int dh);
 
 }  // namespace tir

@@ -7,8 +7,6 @@
 
 namespace tir {
 
-static const int64_t kMax31 = 2147483647LL;
-
 template <int DT, int CT, int DH> static hipError_t launch_append_as(const AppendParams& p, int64_t batch, hipStream_t stream) {
     return launch_kernel(&cache_append_kernel<DT, CT, DH>, dim3((unsigned)(batch * p.touched * p.c.heads), 2), dim3(kAppendThreads), stream, p);
 }
@@ -57,14 +55,6 @@ static tir_status check_cache(const char* who, const tir_kv_cache* c, int64_t ba
     return TIR_OK;
 }
 
-// Strides of rows that are read or written 16 bytes at a time.  `last`: largest index along each; the offsets have to fit 62 bits.
-static tir_status check_strides(const char* who, const char* what, int64_t bs, int64_t rs, int64_t hs) {
-    if (bs < 0 || rs < 0 || hs < 0) return host_error(TIR_ERR_INVALID_ARG, "%s: negative stride of %s", who, what);
-    if ((bs | rs | hs) & 7) return host_error(TIR_ERR_ALIGNMENT, "%s: the strides of %s must be multiples of 8 elements", who, what);
-    if (bs > (1ll << 40) || rs > (1ll << 40) || hs > (1ll << 40)) return host_error(TIR_ERR_UNSUPPORTED, "%s: stride of %s beyond 2^40", who, what);
-    return TIR_OK;
-}
-
 }  // namespace tir
 
 using namespace tir;
@@ -80,8 +70,8 @@ tir_status tir_cache_append(const tir_kv_cache* cache, const void* K, const void
     if (batch < 0 || T < 0) return host_error(TIR_ERR_INVALID_ARG, "negative extent (batch=%lld T=%lld)", (long long)batch, (long long)T);
     AppendParams p = {};
     tir_status st = check_cache(who, cache, batch, &p.c);
-    if (st == TIR_OK) st = check_strides(who, "K", k_bs, k_rs, k_hs);
-    if (st == TIR_OK) st = check_strides(who, "V", v_bs, v_rs, v_hs);
+    if (st == TIR_OK) st = check_row_strides(who, "K", k_bs, k_rs, k_hs);
+    if (st == TIR_OK) st = check_row_strides(who, "V", v_bs, v_rs, v_hs);
     if (st != TIR_OK) return st;
     if (batch == 0 || T == 0) return TIR_OK;
     if (!K || !V || !start) return host_error(TIR_ERR_INVALID_ARG, "%s: K, V or start is null", who);
@@ -115,8 +105,8 @@ tir_status tir_cache_attention(const void* Q, const tir_kv_cache* cache, void* O
     if (batch < 0 || T < 0 || Hq < 0) return host_error(TIR_ERR_INVALID_ARG, "negative extent (batch=%lld T=%lld Hq=%lld)", (long long)batch, (long long)T, (long long)Hq);
     CacheAttnParams p = {};
     tir_status st = check_cache(who, cache, batch, &p.c);
-    if (st == TIR_OK) st = check_strides(who, "Q", q_bs, q_rs, q_hs);
-    if (st == TIR_OK) st = check_strides(who, "O", o_bs, o_rs, o_hs);
+    if (st == TIR_OK) st = check_row_strides(who, "Q", q_bs, q_rs, q_hs);
+    if (st == TIR_OK) st = check_row_strides(who, "O", o_bs, o_rs, o_hs);
     if (st != TIR_OK) return st;
     if (!(scale == scale) || scale > 3.0e38f || scale < -3.0e38f) return host_error(TIR_ERR_INVALID_ARG, "%s: scale must be finite", who);
     if (Hq % p.c.heads) return host_error(TIR_ERR_INVALID_ARG, "%s: %d key heads do not divide %lld query heads", who, p.c.heads, (long long)Hq);
