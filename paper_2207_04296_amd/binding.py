@@ -27,7 +27,7 @@ EXPORTS = ["tir_gemm", "tir_batch_matmul", "tir_conv2d", "tir_last_error", "tir_
            "tir_conv1d", "tir_conv3d", "tir_conv2d_transpose", "tir_debug_force_ksplit", "tir_debug_fastdiv",
            "tir_conv2d_transpose_variant", "tir_conv3d_variant", "tir_tune_conv3d", "tir_tune_conv2d_transpose",
            "tir_workspace_bytes", "tir_set_workspace", "tir_gemm_split_static", "tir_cache_append", "tir_cache_attention",
-           "tir_cross_attention"]
+           "tir_cross_attention", "tir_cross_attention_backward"]
 
 
 class Epilogue(ctypes.Structure):
@@ -163,6 +163,8 @@ def lib() -> ctypes.CDLL:
     L.tir_cache_attention.restype = ci
     L.tir_cross_attention.argtypes = [vp] * 6 + [i64] * 18 + [ctypes.c_float, ci, ci, vp]
     L.tir_cross_attention.restype = ci
+    L.tir_cross_attention_backward.argtypes = [vp] * 11 + [i64] * 18 + [ctypes.c_float, ci, vp]
+    L.tir_cross_attention_backward.restype = ci
     L.tir_tune_batch_matmul.argtypes = [vp, vp, vp] + [i64] * 13 + [ci, ci, pe, ci, pd, vp]
     L.tir_tune_batch_matmul.restype = ci
     L.tir_tune_conv2d.argtypes = [vp, vp, vp] + [i64] * 7 + [ci] * 7 + [ci, ci, pe, ci, pd, vp]
@@ -462,6 +464,21 @@ def tir_cross_attention(Q, K, V, O, lse, lens, batch, M, N, Hq, Hkv, d, q_bs, q_
     """M queries per sequence over lens[b] (None: N) keys of another one; lse (or None): fp32 [batch, Hq, M], for the backward pass."""
     st = (_native or _load_native()).tir_cross_attention(Q, K, V, O, lse, lens, batch, M, N, Hq, Hkv, d, q_bs, q_rs, q_hs, k_bs, k_rs, k_hs, v_bs, v_rs, v_hs,
                                                          o_bs, o_rs, o_hs, scale, in_dtype, out_dtype, stream)
+    if st:
+        _check(st)
+
+
+def tir_cross_attention_backward_status(Q, K, V, O, dO, lse, lens, dQ, dK, dV, delta, batch, M, N, Hq, Hkv, d, q_bs, q_rs, q_hs, k_bs, k_rs, k_hs, v_bs, v_rs, v_hs,
+                                        o_bs, o_rs, o_hs, scale, in_dtype, stream=0) -> int:
+    return lib().tir_cross_attention_backward(*[_ptr(t) for t in (Q, K, V, O, dO, lse, lens, dQ, dK, dV, delta)], batch, M, N, Hq, Hkv, d, q_bs, q_rs, q_hs, k_bs, k_rs, k_hs,
+                                              v_bs, v_rs, v_hs, o_bs, o_rs, o_hs, float(scale), _code(in_dtype), stream)
+
+
+def tir_cross_attention_backward(Q, K, V, O, dO, lse, lens, dQ, dK, dV, delta, batch, M, N, Hq, Hkv, d, q_bs, q_rs, q_hs, k_bs, k_rs, k_hs, v_bs, v_rs, v_hs,
+                                 o_bs, o_rs, o_hs, scale, in_dtype, stream=None) -> None:
+    """Gradients of tir_cross_attention; dQ, dK, dV with the strides of Q, K, V, dO with those of O; delta: fp32 scratch [batch, Hq, M]."""
+    st = (_native or _load_native()).tir_cross_attention_backward(Q, K, V, O, dO, lse, lens, dQ, dK, dV, delta, batch, M, N, Hq, Hkv, d, q_bs, q_rs, q_hs, k_bs, k_rs, k_hs,
+                                                                  v_bs, v_rs, v_hs, o_bs, o_rs, o_hs, scale, in_dtype, stream)
     if st:
         _check(st)
 

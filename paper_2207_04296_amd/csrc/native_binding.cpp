@@ -142,6 +142,7 @@ bool convert(PyObject* o, const tir_epilogue** out, Held& h) { return convert_st
 bool convert(PyObject* o, const tir_kv_cache** out, Held& h) { return convert_struct(o, out, h, g_cache_type, "cache", "instance of KvCache"); }
 bool convert(PyObject* o, const int32_t** out, Held&) { return to_address(o, (void**)out); }
 bool convert(PyObject* o, float** out, Held&) { return to_address(o, (void**)out); }
+bool convert(PyObject* o, const float** out, Held&) { return to_address(o, (void**)out); }
 
 template <class... A, size_t... I>
 PyObject* invoke(tir_status (*fn)(A...), PyObject* const* args, std::index_sequence<I...>) {
@@ -181,6 +182,7 @@ TIR_PY(tir_attention)
 TIR_PY(tir_cache_append)
 TIR_PY(tir_cache_attention)
 TIR_PY(tir_cross_attention)
+TIR_PY(tir_cross_attention_backward)
 #undef TIR_PY
 
 // set_epilogue_type(cls), set_cache_type(cls): called once by the binding, before any operator.
@@ -199,6 +201,7 @@ PyObject* py_set_cache_type(PyObject*, PyObject* cls) { return set_type(cls, &g_
 #define TIR_METHOD(fn) {#fn, (PyCFunction)(void (*)(void))py_##fn, METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {TIR_METHOD(tir_gemm_fused), TIR_METHOD(tir_batch_matmul_fused), TIR_METHOD(tir_conv2d_fused), TIR_METHOD(tir_conv1d),
                           TIR_METHOD(tir_conv3d), TIR_METHOD(tir_conv2d_transpose), TIR_METHOD(tir_attention), TIR_METHOD(tir_cache_append), TIR_METHOD(tir_cache_attention), TIR_METHOD(tir_cross_attention),
+                          TIR_METHOD(tir_cross_attention_backward),
                           {"set_epilogue_type", py_set_epilogue_type, METH_O, nullptr}, {"set_cache_type", py_set_cache_type, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 

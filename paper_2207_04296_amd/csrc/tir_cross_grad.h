@@ -1,0 +1,449 @@
+// Gradients of the attention over another sequence's states.
+//
+// With P = exp(scale * Q K^T - lse), D_i = sum_c dO_ic O_ic (which is sum_j P_ij dP_ij) and dP = dO V^T:
+//     dS = P o (dP - D)     dV = P^T dO     dK = scale * dS^T Q     dQ = scale * dS K
+// Nothing of size M x N meets memory.  Two passes, each of which owns what it sums, so that nothing is added atomically and a result does not depend on
+// timing: one over rows (a workgroup keeps its queries and walks the keys: dQ), one over keys (keeps its keys and walks the queries: dK, dV).
+// S and dP are computed in both: 7 products instead of 5.  Both compute the transposes of S and dP resp. S and dP themselves such that a lane owns one row
+// (one key), as in the forward pass: probabilities and dS come out of the first products in the layout in which the last ones read them.
+//
+// LDS tiles [rows][128 bytes] per 64 channels are read both along their rows (S, dP) and across them (dQ, dK, dV: the transposing read).
+// 16-byte column c of row r is kept at column c ^ (4 * (r/2 mod 2) + r/4 mod 4): the 16 rows of a ds_read_b128 phase meet all banks once, and the 8 rows
+// whose 64-byte segments one transposing read takes lie in both halves of a 128-byte row, the least a 512-byte read can do.
+//
+// Roundings: P and dS are rounded to the input type for the last products.  BF16 has fp32's range.  In F16 a probability is held times 2^14, and dS times a power
+// of two per row (per key) that keeps the largest so far below 2^15: gradients arrive at any magnitude, and dS relative to 1 would fall among F16's subnormals where dQ does not.
+#pragma once
+#include "tir_kernel.h"
+
+namespace tir {
+
+struct GradParams {
+    const void *Q, *K, *V, *O, *dO;
+    void *dQ, *dK, *dV;
+    const float* lse;        // [batch][query heads][M]
+    float* delta;            // the same: D, written by the pass over rows
+    const int* lens;         // null: N each
+    long long q_bs, q_rs, q_hs, k_bs, k_rs, k_hs, v_bs, v_rs, v_hs, o_bs, o_rs, o_hs;
+    int M, N, heads, G;      // key heads, query heads per key head
+    int batch, tiles;        // tiles of rows resp. keys of a (sequence, key head)
+    int slices;              // workgroups that share a tile's walk: partial sums in ws, added by grad_sum_kernel
+    float scale, scale_log2e;
+    float* ws;
+    unsigned div_h_magic, div_g_magic, div_tiles_magic;
+    int div_h_shift, div_g_shift, div_tiles_shift;
+};
+
+constexpr int kGradWaves = 4, kGradThreads = 64 * kGradWaves, kGradTile = 32 * kGradWaves;      // rows resp. keys of a workgroup
+constexpr int kGradChunk = 64;      // keys resp. rows of a step
+
+hipError_t launch_grad_rows(const GradParams& p, int dt, int dh, hipStream_t stream);
+hipError_t launch_grad_keys(const GradParams& p, int dt, int dh, hipStream_t stream);
+
+__device__ __forceinline__ int grad_swz(int row) { return ((row & 2) << 1) | ((row >> 2) & 3); }
+
+// One wave's part of a workgroup's copy of RB rows of DH channels into an LDS tile.
+template <int DH, int RB> struct GradTile {
+    static constexpr int HALVES = DH / 64, HALF = RB * 128, BYTES = HALVES * HALF, ROW = DH * 2;
+    static constexpr int PASSES = RB / (8 * kGradWaves);      // of 8 rows per wave and half
+    static_assert(PASSES >= 1, "");
+    static __device__ __forceinline__ unsigned lane_offset(int wave, int lane, int rs) {      // (rs in elements)
+        const int row = wave * 8 + (lane >> 3);
+        return (unsigned)(row * rs * 2 + (((lane & 7) ^ grad_swz(row)) << 4));
+    }
+    static __device__ __forceinline__ void copy(char* tile, const char* base, int left, int rs, unsigned off, int wave) {
+        const i32x4 r = make_rsrc(base, left > 0 ? (long long)(left - 1) * rs * 2 + ROW : 0);
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+            for (int u = 0; u < PASSES; ++u) load_to_lds_at(r, tile + h * HALF + (u * kGradWaves + wave) * 1024, off, u * kGradWaves * 8 * rs * 2 + h * 128);
+    }
+    // Operand of k-step ks (16 channels): row l31 of the 32 from row r0
+    static __device__ __forceinline__ uint4 along(const char* tile, int r0, int ks, int l31, int g) {
+        return *(const uint4*)(tile + (ks >> 2) * HALF + (r0 + l31) * 128 + ((((ks & 3) * 2 + g) ^ grad_swz(l31)) << 4));
+    }
+    // Operand of the 16 rows from r0 for channels 32*db ..: position (g, 4*hh + e) is row r0 + 8*hh + 4*g + e, the order of a product's result registers
+    static __device__ __forceinline__ uint4 across(const char* tile, int r0, int db, int blk, int s16) {
+        i16x4 h[2];
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) {
+            const int row = hh * 8 + 4 * (blk >> 1) + (s16 >> 2);
+            const int col = (db & 1) * 4 + 2 * (blk & 1) + ((s16 & 3) >> 1);
+            const char* const ptr = tile + (db >> 1) * HALF + (r0 + row) * 128 + ((col ^ grad_swz(row)) << 4) + (s16 & 1) * 8;
+            h[hh] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(TIR_LDS_PTR(i16x4, ptr));
+        }
+        const i32x2 lo = __builtin_bit_cast(i32x2, h[0]), hi = __builtin_bit_cast(i32x2, h[1]);
+        return make_uint4((unsigned)lo[0], (unsigned)lo[1], (unsigned)hi[0], (unsigned)hi[1]);
+    }
+};
+
+// 64 consecutive floats from a descriptor into LDS, one per lane.
+__device__ __forceinline__ void floats_to_lds(const i32x4& rsrc, const char* lds_base, unsigned voffset) {
+    const unsigned lds_addr = (unsigned)(unsigned long long)TIR_LDS_PTR(const char, lds_base);
+    asm volatile(
+        "s_mov_b32 m0, %0\n\t"
+        "s_nop 0\n\t"
+        "buffer_load_dword %1, %2, 0 offen lds"
+        :
+        : "s"(lds_addr), "v"(voffset), "s"(rsrc)
+        : "memory", "m0");
+}
+
+template <int DT> __device__ __forceinline__ unsigned grad_pack(float a, float b) {
+    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    if constexpr (DT == DT_F16) {
+        const h2 v = {(_Float16)a, (_Float16)b};
+        return __builtin_bit_cast(unsigned, v);
+    } else {
+        const b2 v = {(__bf16)a, (__bf16)b};
+        return __builtin_bit_cast(unsigned, v);
+    }
+}
+// Sum of the products of two operands' eight values.
+template <int DT> __device__ __forceinline__ float dot8(const uint4& a, const uint4& b) {
+    const unsigned x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float u[2], v[2];
+        if constexpr (DT == DT_F16) {
+            typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+            const h2 p = __builtin_bit_cast(h2, x[i]), q = __builtin_bit_cast(h2, y[i]);
+            u[0] = (float)p[0]; u[1] = (float)p[1];
+            v[0] = (float)q[0]; v[1] = (float)q[1];
+        } else {
+            u[0] = __builtin_bit_cast(float, x[i] << 16); u[1] = __builtin_bit_cast(float, x[i] & 0xffff0000u);
+            v[0] = __builtin_bit_cast(float, y[i] << 16); v[1] = __builtin_bit_cast(float, y[i] & 0xffff0000u);
+        }
+        s = __builtin_fmaf(u[0], v[0], s);
+        s = __builtin_fmaf(u[1], v[1], s);
+    }
+    return s;
+}
+__device__ __forceinline__ float grad_half_max(float x) {      // over the two half-waves
+    const auto both = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+    const unsigned lo = both[0], hi = both[1];
+    return __builtin_fmaxf(__builtin_bit_cast(float, lo), __builtin_bit_cast(float, hi));
+}
+
+// dS of 32 x 32 pairs, rounded for the last product.  `by`: the power of two that a lane's row (key) is held times; where it shrinks, so do the sums in acc.
+template <int DT, int DB> __device__ __forceinline__ void round_ds(f32x16& ds, float& by, f32x16 (&acc)[DB], unsigned (&w)[8]) {
+    if constexpr (DT == DT_F16) {
+        float top = 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = __builtin_fmaxf(top, __builtin_fabsf(ds[r]));
+        top = grad_half_max(top);
+        if (__builtin_amdgcn_ballot_w64(top * by >= 0x1p15f) != 0) {
+            // 2^(14 - e) with top < 2^e: below 2^14, and room for twice as much to come (an infinite or NaN dS: the factor stays, the result shows it)
+            const float fresh = __builtin_amdgcn_ldexpf(1.f, 14 - __builtin_amdgcn_frexp_expf(top));
+            const float next = top * by >= 0x1p15f && top < __builtin_inff() ? fresh : by;
+            const float f = next / by;
+            by = next;
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[db][r] *= f;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = grad_pack<DT>(ds[2 * i] * by, ds[2 * i + 1] * by);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = grad_pack<DT>(ds[2 * i], ds[2 * i + 1]);
+    }
+}
+constexpr float kFirstFactor = 0x1p100f;      // before any dS has been seen
+template <int DT> __device__ __forceinline__ float p_factor_log2() { return DT == DT_F16 ? 14.f : 0.f; }
+
+// ---------------------------------------------------------------------------------------------
+// dQ: four waves of 32 rows (position, query head) each; keys and values through two LDS stages.
+// ---------------------------------------------------------------------------------------------
+template <int DT, int DH>
+__global__ void __launch_bounds__(kGradThreads, 2) grad_rows_kernel(const GradParams p) {
+    typedef GradTile<DH, kGradChunk> T;
+    constexpr int KSTEPS = DH / 16, DB = DH / 32, STAGE = 2 * T::BYTES;
+    static_assert(2 * STAGE >= kGradTile * DH * 2, "the output tile is staged in the rings");
+    __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
+    const int lane = threadIdx.x & 63, l31 = lane & 31, g = lane >> 5, blk = lane >> 4, s16 = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int bh = (int)fastdiv(blockIdx.x, p.div_tiles_magic, p.div_tiles_shift);
+    const int row0 = ((int)blockIdx.x - bh * p.tiles) * kGradTile;
+    const int b = (int)fastdiv((unsigned)bh, p.div_h_magic, p.div_h_shift), h = bh - b * p.heads;
+    const int rows = p.M * p.G - row0 < kGradTile ? p.M * p.G - row0 : kGradTile;
+    int n = p.N;
+    if (p.lens) {
+        n = p.lens[b];
+        n = n < 0 ? 0 : (n > p.N ? p.N : n);
+    }
+    const int chunks_all = (n + kGradChunk - 1) / kGradChunk;
+    const int per = (chunks_all + p.slices - 1) / p.slices;
+    const int c0 = (int)blockIdx.y * per;
+    const int chunks = chunks_all - c0 < per ? chunks_all - c0 : per;      // may be none: this slice's sums are zeros
+
+    const char* const Kb = (const char*)p.K + 2 * (b * p.k_bs + h * p.k_hs);
+    const char* const Vb = (const char*)p.V + 2 * (b * p.v_bs + h * p.v_hs);
+    const int k_rs = (int)p.k_rs, v_rs = (int)p.v_rs;
+    const unsigned k_off = T::lane_offset(wave, lane, k_rs), v_off = T::lane_offset(wave, lane, v_rs);
+    auto copy = [&](int i) __attribute__((always_inline)) {
+        char* const st = smem + (i & 1) * STAGE;
+        const long long key = (long long)(c0 + i) * kGradChunk;
+        const int left = i < chunks ? n - (int)key : 0;
+        T::copy(st, Kb + key * k_rs * 2, left, k_rs, k_off, wave);
+        T::copy(st + T::BYTES, Vb + key * v_rs * 2, left, v_rs, v_off, wave);
+    };
+    if (chunks > 0) copy(0);
+
+    // this lane's row
+    const int row = row0 + wave * 32 + l31;
+    const bool live = wave * 32 + l31 < rows;
+    const int m = (int)fastdiv((unsigned)row, p.div_g_magic, p.div_g_shift), hq = h * p.G + row - m * p.G;
+    uint4 qf[KSTEPS], of[KSTEPS];
+    float delta = 0.f, lse2 = 0.f;
+    const long long stat = ((long long)b * p.heads * p.G + hq) * p.M + m;
+#pragma unroll
+    for (int ks = 0; ks < KSTEPS; ++ks) qf[ks] = of[ks] = make_uint4(0, 0, 0, 0);
+    if (live) {
+        const char* const q = (const char*)p.Q + 2 * (b * p.q_bs + m * p.q_rs + hq * p.q_hs) + g * 16;
+        const char* const go = (const char*)p.dO + 2 * (b * p.o_bs + m * p.o_rs + hq * p.o_hs) + g * 16;
+        const char* const o = (const char*)p.O + 2 * (b * p.o_bs + m * p.o_rs + hq * p.o_hs) + g * 16;
+#pragma unroll
+        for (int ks = 0; ks < KSTEPS; ++ks) {
+            qf[ks] = *(const uint4*)(q + ks * 32);
+            of[ks] = *(const uint4*)(go + ks * 32);
+            delta += dot8<DT>(of[ks], *(const uint4*)(o + ks * 32));
+        }
+        lse2 = p.lse[stat] * 1.44269504088896340736f;
+    }
+    delta += __shfl_xor(delta, 32);
+    if (live && g == 0 && blockIdx.y == 0) p.delta[stat] = delta;
+
+    f32x16 acc[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[db][r] = 0.f;
+    float by = DT == DT_F16 ? kFirstFactor : 1.f;
+    const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+
+    for (int i = 0; i < chunks; ++i) {
+        copy_barrier<0>();                     // chunk i is in, and everybody is past chunk i - 1
+        if (i + 1 < chunks) copy(i + 1);
+        const char* const tk = smem + (i & 1) * STAGE;
+        const char* const tv = tk + T::BYTES;
+#pragma unroll
+        for (int jb = 0; jb < kGradChunk / 32; ++jb) {
+            f32x16 s, dp;
+#pragma unroll
+            for (int ks = 0; ks < KSTEPS; ++ks) s = InTraits<DT>::mfma(T::along(tk, jb * 32, ks, l31, g), qf[ks], ks == 0 ? zero16 : s);
+#pragma unroll
+            for (int ks = 0; ks < KSTEPS; ++ks) dp = InTraits<DT>::mfma(T::along(tv, jb * 32, ks, l31, g), of[ks], ks == 0 ? zero16 : dp);
+            const int left = n - (c0 + i) * kGradChunk - jb * 32;      // keys of this block
+            f32x16 ds;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) ds[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], p.scale_log2e, -lse2)) * (dp[r] - delta);
+            if (left < 32) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) ds[r] = 8 * (r >> 2) + 4 * g + (r & 3) < left ? ds[r] : 0.f;
+            }
+            unsigned w[8];
+            round_ds<DT, DB>(ds, by, acc, w);
+#pragma unroll
+            for (int ss = 0; ss < 2; ++ss) {
+                const uint4 df = make_uint4(w[4 * ss], w[4 * ss + 1], w[4 * ss + 2], w[4 * ss + 3]);
+#pragma unroll
+                for (int db = 0; db < DB; ++db) acc[db] = InTraits<DT>::mfma(T::across(tk, jb * 32 + ss * 16, db, blk, s16), df, acc[db]);
+            }
+            TIR_FENCE();                       // (the next block's operands read ahead of here would not fit the registers)
+        }
+    }
+    const float f = p.scale / by;
+    if (p.slices > 1) {
+        // [tile][slice][wave][db][quarter][lane] of four values
+        typedef float f32x4 __attribute__((ext_vector_type(4)));
+        f32x4* const o = (f32x4*)p.ws + ((long long)blockIdx.x * p.slices + blockIdx.y) * (kGradTile * DH / 4) + wave * (32 * DH / 4) + lane;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4) o[(db * 4 + q4) * 64] = f32x4{acc[db][4 * q4] * f, acc[db][4 * q4 + 1] * f, acc[db][4 * q4 + 2] * f, acc[db][4 * q4 + 3] * f};
+        return;
+    }
+    if (!live) return;
+    unsigned short* const out = (unsigned short*)p.dQ + b * p.q_bs + m * p.q_rs + hq * p.q_hs;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4)
+            *(uint2*)(out + db * 32 + q4 * 8 + 4 * g) = make_uint2(grad_pack<DT>(acc[db][4 * q4] * f, acc[db][4 * q4 + 1] * f), grad_pack<DT>(acc[db][4 * q4 + 2] * f, acc[db][4 * q4 + 3] * f));
+}
+
+// ---------------------------------------------------------------------------------------------
+// dK and dV: four waves of 32 keys each; queries and dO, head after head, through two LDS stages with their lse and D.
+// ---------------------------------------------------------------------------------------------
+template <int DT, int DH>
+__global__ void __launch_bounds__(kGradThreads, DH == 64 ? 2 : 1) grad_keys_kernel(const GradParams p) {
+    typedef GradTile<DH, kGradChunk> T;
+    constexpr int KSTEPS = DH / 16, DB = DH / 32, STAGE = 2 * T::BYTES + 2 * kGradChunk * 4;
+    __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
+    const int lane = threadIdx.x & 63, l31 = lane & 31, g = lane >> 5, blk = lane >> 4, s16 = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int bh = (int)fastdiv(blockIdx.x, p.div_tiles_magic, p.div_tiles_shift);
+    const int key0 = ((int)blockIdx.x - bh * p.tiles) * kGradTile;
+    const int b = (int)fastdiv((unsigned)bh, p.div_h_magic, p.div_h_shift), h = bh - b * p.heads;
+    int n = p.N;
+    if (p.lens) {
+        n = p.lens[b];
+        n = n < 0 ? 0 : (n > p.N ? p.N : n);
+    }
+    const int key = key0 + wave * 32 + l31;
+    const bool live = key < n;
+    // this slice's chunks of rows, of all query heads one after the other; none where the tile has no key
+    const int head_chunks = (p.M + kGradChunk - 1) / kGradChunk;
+    const int all = key0 < n ? head_chunks * p.G : 0;
+    const int per = (all + p.slices - 1) / p.slices;
+    const int c0 = (int)blockIdx.y * per;
+    const int chunks = all - c0 < per ? all - c0 : per;
+
+    const int q_rs = (int)p.q_rs, o_rs = (int)p.o_rs;
+    const unsigned q_off = T::lane_offset(wave, lane, q_rs), o_off = T::lane_offset(wave, lane, o_rs);
+    int head_at = c0 / (head_chunks > 0 ? head_chunks : 1), chunk_at = c0 - head_at * head_chunks;      // of the next copy
+    auto copy = [&](int st_at) __attribute__((always_inline)) {
+        char* const st = smem + st_at * STAGE;
+        const int hq = h * p.G + head_at, m = chunk_at * kGradChunk, left = p.M - m;
+        T::copy(st, (const char*)p.Q + 2 * (b * p.q_bs + (long long)m * q_rs + hq * p.q_hs), left, q_rs, q_off, wave);
+        T::copy(st + T::BYTES, (const char*)p.dO + 2 * (b * p.o_bs + (long long)m * o_rs + hq * p.o_hs), left, o_rs, o_off, wave);
+        const long long stat = ((long long)b * p.heads * p.G + hq) * p.M + m;
+        if (wave < 2) floats_to_lds(make_rsrc((wave ? p.delta : p.lse) + stat, (long long)left * 4), st + 2 * T::BYTES + wave * (kGradChunk * 4), (unsigned)lane * 4);
+        if (++chunk_at == head_chunks) {
+            chunk_at = 0;
+            ++head_at;
+        }
+    };
+    if (chunks > 0) copy(0);
+
+    uint4 kf[KSTEPS], vf[KSTEPS];
+#pragma unroll
+    for (int ks = 0; ks < KSTEPS; ++ks) kf[ks] = vf[ks] = make_uint4(0, 0, 0, 0);
+    if (live) {
+        const char* const k = (const char*)p.K + 2 * (b * p.k_bs + key * p.k_rs + h * p.k_hs) + g * 16;
+        const char* const v = (const char*)p.V + 2 * (b * p.v_bs + key * p.v_rs + h * p.v_hs) + g * 16;
+#pragma unroll
+        for (int ks = 0; ks < KSTEPS; ++ks) {
+            kf[ks] = *(const uint4*)(k + ks * 32);
+            vf[ks] = *(const uint4*)(v + ks * 32);
+        }
+    }
+    f32x16 dk[DB], dv[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dk[db][r] = dv[db][r] = 0.f;
+    float by = DT == DT_F16 ? kFirstFactor : 1.f;
+    const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+    for (int i = 0; i < chunks; ++i) {
+        copy_barrier<0>();
+        if (i + 1 < chunks) copy((i + 1) & 1);
+        const char* const tq = smem + (i & 1) * STAGE;
+        const char* const to = tq + T::BYTES;
+#pragma unroll
+        for (int ib = 0; ib < kGradChunk / 32; ++ib) {
+            f32x16 s, dp;
+#pragma unroll
+            for (int ks = 0; ks < KSTEPS; ++ks) s = InTraits<DT>::mfma(T::along(tq, ib * 32, ks, l31, g), kf[ks], ks == 0 ? zero16 : s);
+#pragma unroll
+            for (int ks = 0; ks < KSTEPS; ++ks) dp = InTraits<DT>::mfma(T::along(to, ib * 32, ks, l31, g), vf[ks], ks == 0 ? zero16 : dp);
+            // row 8*a + 4*g + e of the block is register 4*a + e.  Rows behind the last read zeros: P = 1 there, dO and dS are 0.
+            unsigned pw[8], w[8];
+            f32x16 ds;
+#pragma unroll
+            for (int a = 0; a < 4; ++a) {
+                const f32x4 l4 = *(const f32x4*)(to + T::BYTES + (ib * 32 + 8 * a + 4 * g) * 4);
+                const f32x4 d4 = *(const f32x4*)(to + T::BYTES + kGradChunk * 4 + (ib * 32 + 8 * a + 4 * g) * 4);
+                float pr[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float t = __builtin_fmaf(s[4 * a + e], p.scale_log2e, l4[e] * -1.44269504088896340736f);
+                    pr[e] = __builtin_amdgcn_exp2f(t);
+                    ds[4 * a + e] = pr[e] * (dp[4 * a + e] - d4[e]);
+                    pr[e] = DT == DT_F16 ? pr[e] * 0x1p14f : pr[e];
+                }
+                pw[2 * a] = grad_pack<DT>(pr[0], pr[1]);
+                pw[2 * a + 1] = grad_pack<DT>(pr[2], pr[3]);
+            }
+#pragma unroll
+            for (int ss = 0; ss < 2; ++ss) {
+                const uint4 pf = make_uint4(pw[4 * ss], pw[4 * ss + 1], pw[4 * ss + 2], pw[4 * ss + 3]);
+#pragma unroll
+                for (int db = 0; db < DB; ++db) dv[db] = InTraits<DT>::mfma(T::across(to, ib * 32 + ss * 16, db, blk, s16), pf, dv[db]);
+            }
+            round_ds<DT, DB>(ds, by, dk, w);
+#pragma unroll
+            for (int ss = 0; ss < 2; ++ss) {
+                const uint4 df = make_uint4(w[4 * ss], w[4 * ss + 1], w[4 * ss + 2], w[4 * ss + 3]);
+#pragma unroll
+                for (int db = 0; db < DB; ++db) dk[db] = InTraits<DT>::mfma(T::across(tq, ib * 32 + ss * 16, db, blk, s16), df, dk[db]);
+            }
+        }
+    }
+    const float fk = p.scale / by, fv = DT == DT_F16 ? 0x1p-14f : 1.f;
+    if (p.slices > 1) {
+        f32x4* const o = (f32x4*)p.ws + ((long long)blockIdx.x * p.slices + blockIdx.y) * (2 * kGradTile * DH / 4) + wave * (32 * DH / 4) + lane;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4) {
+                o[(db * 4 + q4) * 64] = f32x4{dk[db][4 * q4] * fk, dk[db][4 * q4 + 1] * fk, dk[db][4 * q4 + 2] * fk, dk[db][4 * q4 + 3] * fk};
+                o[(db * 4 + q4) * 64 + kGradTile * DH / 4] = f32x4{dv[db][4 * q4] * fv, dv[db][4 * q4 + 1] * fv, dv[db][4 * q4 + 2] * fv, dv[db][4 * q4 + 3] * fv};
+            }
+        return;
+    }
+    if (key >= p.N) return;
+    unsigned short* const ok = (unsigned short*)p.dK + b * p.k_bs + key * p.k_rs + h * p.k_hs;
+    unsigned short* const ov = (unsigned short*)p.dV + b * p.v_bs + key * p.v_rs + h * p.v_hs;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+            const int at = db * 32 + q4 * 8 + 4 * g;
+            const uint2 x = make_uint2(grad_pack<DT>(dk[db][4 * q4] * fk, dk[db][4 * q4 + 1] * fk), grad_pack<DT>(dk[db][4 * q4 + 2] * fk, dk[db][4 * q4 + 3] * fk));
+            const uint2 y = make_uint2(grad_pack<DT>(dv[db][4 * q4] * fv, dv[db][4 * q4 + 1] * fv), grad_pack<DT>(dv[db][4 * q4 + 2] * fv, dv[db][4 * q4 + 3] * fv));
+            *(uint2*)(ok + at) = live ? x : make_uint2(0, 0);
+            *(uint2*)(ov + at) = live ? y : make_uint2(0, 0);
+        }
+}
+
+// ---------------------------------------------------------------------------------------------
+// The slices' partial sums, added in slice order: one thread per four values of a tile.  KEYS: dK (the first half of a partial) and dV.
+// ---------------------------------------------------------------------------------------------
+template <int DT, int DH, bool KEYS> __global__ void __launch_bounds__(256) grad_sum_kernel(const GradParams p) {
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
+    constexpr int PART = (KEYS ? 2 : 1) * kGradTile * DH / 4;
+    const int tile = (int)blockIdx.y, at = (int)(blockIdx.x * 256 + threadIdx.x);      // < PART: a multiple of 256
+    const f32x4* const part = (const f32x4*)p.ws + (long long)tile * p.slices * PART + at;
+    f32x4 sum = part[0];
+    for (int z = 1; z < p.slices; ++z) sum += part[(long long)z * PART];
+    const int bh = (int)fastdiv((unsigned)tile, p.div_tiles_magic, p.div_tiles_shift);
+    const int b = (int)fastdiv((unsigned)bh, p.div_h_magic, p.div_h_shift), h = bh - b * p.heads;
+    const int in = at % (kGradTile * DH / 4), lane = in & 63, grp = in >> 6;       // grp = wave * (DH / 8) + db * 4 + quarter
+    const int row = (tile - bh * p.tiles) * kGradTile + grp / (DH / 8) * 32 + (lane & 31);
+    const int ch = grp % (DH / 8) * 8 + 4 * (lane >> 5);
+    const uint2 v = make_uint2(grad_pack<DT>(sum[0], sum[1]), grad_pack<DT>(sum[2], sum[3]));
+    if constexpr (KEYS) {
+        if (row >= p.N) return;
+        int n = p.N;
+        if (p.lens) {
+            n = p.lens[b];
+            n = n < 0 ? 0 : (n > p.N ? p.N : n);
+        }
+        const bool second = at >= kGradTile * DH / 4;
+        unsigned short* const o = second ? (unsigned short*)p.dV + b * p.v_bs + row * p.v_rs + h * p.v_hs : (unsigned short*)p.dK + b * p.k_bs + row * p.k_rs + h * p.k_hs;
+        *(uint2*)(o + ch) = row < n ? v : make_uint2(0, 0);
+    } else {
+        if (row >= p.M * p.G) return;
+        const int m = (int)fastdiv((unsigned)row, p.div_g_magic, p.div_g_shift), hq = h * p.G + row - m * p.G;
+        *(uint2*)((unsigned short*)p.dQ + b * p.q_bs + m * p.q_rs + hq * p.q_hs + ch) = v;
+    }
+}
+
+}  // namespace tir
