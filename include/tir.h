@@ -260,7 +260,7 @@ tir_status tir_cross_attention(const void* Q, const void* K, const void* V, void
 
 /*
  * Gradients of tir_cross_attention: Q, K, V, lens, extents, strides and scale as in the forward call, O and lse its results (O in the input type), dO the gradient that
- * arrives, with O's strides.  With P_ij = exp(scale * Q_i . K_j - lse_i) over j < lens[b], D_i = dO_i . O_i:
+ * arrives, with strides g_bs, g_rs and g_hs of its own.  With P_ij = exp(scale * Q_i . K_j - lse_i) over j < lens[b], D_i = dO_i . O_i:
  *     dV_j = sum_i P_ij dO_i     dS_ij = P_ij (dO_i . V_j - D_i)     dQ_i = scale * sum_j dS_ij K_j     dK_j = scale * sum_i dS_ij Q_i
  * the sums of dK and dV running over all query heads that share the key head as well.  dQ has Q's type and strides, dK and dV those of K and V; they are fully overwritten: rows of dK and
  * dV from lens[b] on are zeros, as are the rows of dQ of a sequence without keys.  A stride of Q, K or V that is 0 along an axis of more than one is refused: the gradients would overlap
@@ -274,8 +274,8 @@ tir_status tir_cross_attention_backward(const void* Q, const void* K, const void
                                         float* delta, int64_t batch, int64_t M, int64_t N, int64_t Hq, int64_t Hkv,
                                         int64_t d, int64_t q_bs, int64_t q_rs, int64_t q_hs, int64_t k_bs,
                                         int64_t k_rs, int64_t k_hs, int64_t v_bs, int64_t v_rs, int64_t v_hs,
-                                        int64_t o_bs, int64_t o_rs, int64_t o_hs, float scale, tir_dtype in,
-                                        tir_stream stream);
+                                        int64_t o_bs, int64_t o_rs, int64_t o_hs, int64_t g_bs, int64_t g_rs,
+                                        int64_t g_hs, float scale, tir_dtype in, tir_stream stream);
 
 /* Message for the calling thread's last failed call ("" if none).  Never NULL; valid until the
  * thread's next failing call. */

@@ -163,7 +163,7 @@ def lib() -> ctypes.CDLL:
     L.tir_cache_attention.restype = ci
     L.tir_cross_attention.argtypes = [vp] * 6 + [i64] * 18 + [ctypes.c_float, ci, ci, vp]
     L.tir_cross_attention.restype = ci
-    L.tir_cross_attention_backward.argtypes = [vp] * 11 + [i64] * 18 + [ctypes.c_float, ci, vp]
+    L.tir_cross_attention_backward.argtypes = [vp] * 11 + [i64] * 21 + [ctypes.c_float, ci, vp]
     L.tir_cross_attention_backward.restype = ci
     L.tir_tune_batch_matmul.argtypes = [vp, vp, vp] + [i64] * 13 + [ci, ci, pe, ci, pd, vp]
     L.tir_tune_batch_matmul.restype = ci
@@ -469,16 +469,16 @@ def tir_cross_attention(Q, K, V, O, lse, lens, batch, M, N, Hq, Hkv, d, q_bs, q_
 
 
 def tir_cross_attention_backward_status(Q, K, V, O, dO, lse, lens, dQ, dK, dV, delta, batch, M, N, Hq, Hkv, d, q_bs, q_rs, q_hs, k_bs, k_rs, k_hs, v_bs, v_rs, v_hs,
-                                        o_bs, o_rs, o_hs, scale, in_dtype, stream=0) -> int:
+                                        o_bs, o_rs, o_hs, g_bs, g_rs, g_hs, scale, in_dtype, stream=0) -> int:
     return lib().tir_cross_attention_backward(*[_ptr(t) for t in (Q, K, V, O, dO, lse, lens, dQ, dK, dV, delta)], batch, M, N, Hq, Hkv, d, q_bs, q_rs, q_hs, k_bs, k_rs, k_hs,
-                                              v_bs, v_rs, v_hs, o_bs, o_rs, o_hs, float(scale), _code(in_dtype), stream)
+                                              v_bs, v_rs, v_hs, o_bs, o_rs, o_hs, g_bs, g_rs, g_hs, float(scale), _code(in_dtype), stream)
 
 
 def tir_cross_attention_backward(Q, K, V, O, dO, lse, lens, dQ, dK, dV, delta, batch, M, N, Hq, Hkv, d, q_bs, q_rs, q_hs, k_bs, k_rs, k_hs, v_bs, v_rs, v_hs,
-                                 o_bs, o_rs, o_hs, scale, in_dtype, stream=None) -> None:
-    """Gradients of tir_cross_attention; dQ, dK, dV with the strides of Q, K, V, dO with those of O; delta: fp32 scratch [batch, Hq, M]."""
+                                 o_bs, o_rs, o_hs, g_bs, g_rs, g_hs, scale, in_dtype, stream=None) -> None:
+    """Gradients of tir_cross_attention; dQ, dK, dV with the strides of Q, K, V, dO with its own (g_*); delta: fp32 scratch [batch, Hq, M]."""
     st = (_native or _load_native()).tir_cross_attention_backward(Q, K, V, O, dO, lse, lens, dQ, dK, dV, delta, batch, M, N, Hq, Hkv, d, q_bs, q_rs, q_hs, k_bs, k_rs, k_hs,
-                                                                  v_bs, v_rs, v_hs, o_bs, o_rs, o_hs, scale, in_dtype, stream)
+                                                                  v_bs, v_rs, v_hs, o_bs, o_rs, o_hs, g_bs, g_rs, g_hs, scale, in_dtype, stream)
     if st:
         _check(st)
 

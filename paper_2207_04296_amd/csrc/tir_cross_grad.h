@@ -24,7 +24,7 @@ struct GradParams {
     const float* lse;        // [batch][query heads][M]
     float* delta;            // the same: D, written by the pass over rows
     const int* lens;         // null: N each
-    long long q_bs, q_rs, q_hs, k_bs, k_rs, k_hs, v_bs, v_rs, v_hs, o_bs, o_rs, o_hs;
+    long long q_bs, q_rs, q_hs, k_bs, k_rs, k_hs, v_bs, v_rs, v_hs, o_bs, o_rs, o_hs, g_bs, g_rs, g_hs;      // (g: dO)
     int M, N, heads, G;      // key heads, query heads per key head
     int batch, tiles;        // tiles of rows resp. keys of a (sequence, key head)
     int slices;              // workgroups that share a tile's walk: partial sums in ws, added by grad_sum_kernel
@@ -204,7 +204,7 @@ __global__ void __launch_bounds__(kGradThreads, 2) grad_rows_kernel(const GradPa
     for (int ks = 0; ks < KSTEPS; ++ks) qf[ks] = of[ks] = make_uint4(0, 0, 0, 0);
     if (live) {
         const char* const q = (const char*)p.Q + 2 * (b * p.q_bs + m * p.q_rs + hq * p.q_hs) + g * 16;
-        const char* const go = (const char*)p.dO + 2 * (b * p.o_bs + m * p.o_rs + hq * p.o_hs) + g * 16;
+        const char* const go = (const char*)p.dO + 2 * (b * p.g_bs + m * p.g_rs + hq * p.g_hs) + g * 16;
         const char* const o = (const char*)p.O + 2 * (b * p.o_bs + m * p.o_rs + hq * p.o_hs) + g * 16;
 #pragma unroll
         for (int ks = 0; ks < KSTEPS; ++ks) {
@@ -303,14 +303,14 @@ __global__ void __launch_bounds__(kGradThreads, DH == 64 ? 2 : 1) grad_keys_kern
     const int c0 = (int)blockIdx.y * per;
     const int chunks = all - c0 < per ? all - c0 : per;
 
-    const int q_rs = (int)p.q_rs, o_rs = (int)p.o_rs;
-    const unsigned q_off = T::lane_offset(wave, lane, q_rs), o_off = T::lane_offset(wave, lane, o_rs);
+    const int q_rs = (int)p.q_rs, go_rs = (int)p.g_rs;
+    const unsigned q_off = T::lane_offset(wave, lane, q_rs), go_off = T::lane_offset(wave, lane, go_rs);
     int head_at = c0 / (head_chunks > 0 ? head_chunks : 1), chunk_at = c0 - head_at * head_chunks;      // of the next copy
     auto copy = [&](int st_at) __attribute__((always_inline)) {
         char* const st = smem + st_at * STAGE;
         const int hq = h * p.G + head_at, m = chunk_at * kGradChunk, left = p.M - m;
         T::copy(st, (const char*)p.Q + 2 * (b * p.q_bs + (long long)m * q_rs + hq * p.q_hs), left, q_rs, q_off, wave);
-        T::copy(st + T::BYTES, (const char*)p.dO + 2 * (b * p.o_bs + (long long)m * o_rs + hq * p.o_hs), left, o_rs, o_off, wave);
+        T::copy(st + T::BYTES, (const char*)p.dO + 2 * (b * p.g_bs + (long long)m * go_rs + hq * p.g_hs), left, go_rs, go_off, wave);
         const long long stat = ((long long)b * p.heads * p.G + hq) * p.M + m;
         if (wave < 2) floats_to_lds(make_rsrc((wave ? p.delta : p.lse) + stat, (long long)left * 4), st + 2 * T::BYTES + wave * (kGradChunk * 4), (unsigned)lane * 4);
         if (++chunk_at == head_chunks) {

@@ -43,8 +43,8 @@ tir_status tir_cross_attention_backward(const void* Q, const void* K, const void
                                         float* delta, int64_t batch, int64_t M, int64_t N, int64_t Hq, int64_t Hkv,
                                         int64_t d, int64_t q_bs, int64_t q_rs, int64_t q_hs, int64_t k_bs,
                                         int64_t k_rs, int64_t k_hs, int64_t v_bs, int64_t v_rs, int64_t v_hs,
-                                        int64_t o_bs, int64_t o_rs, int64_t o_hs, float scale, tir_dtype in,
-                                        tir_stream stream) {
+                                        int64_t o_bs, int64_t o_rs, int64_t o_hs, int64_t g_bs, int64_t g_rs,
+                                        int64_t g_hs, float scale, tir_dtype in, tir_stream stream) {
     const char* const who = "cross attention backward";
     if ((int)in < 0 || (int)in > TIR_E4M3) return host_error(TIR_ERR_INVALID_ARG, "unknown dtype code (in=%d)", (int)in);
     if (in != TIR_F16 && in != TIR_BF16) return host_error(TIR_ERR_UNSUPPORTED, "%s: unsupported dtype %d", who, (int)in);
@@ -53,6 +53,7 @@ tir_status tir_cross_attention_backward(const void* Q, const void* K, const void
     if (st == TIR_OK) st = check_row_strides(who, "K", k_bs, k_rs, k_hs);
     if (st == TIR_OK) st = check_row_strides(who, "V", v_bs, v_rs, v_hs);
     if (st == TIR_OK) st = check_row_strides(who, "O", o_bs, o_rs, o_hs);
+    if (st == TIR_OK) st = check_row_strides(who, "dO", g_bs, g_rs, g_hs);
     if (st != TIR_OK) return st;
     if (batch == 0 || Hq == 0) return TIR_OK;
     if ((batch > 1 && q_bs == 0) || (M > 1 && q_rs == 0) || (Hq > 1 && q_hs == 0)) return host_error(TIR_ERR_INVALID_ARG, "%s: a stride of Q is zero: the gradients of its rows overlap", who);
@@ -72,6 +73,7 @@ tir_status tir_cross_attention_backward(const void* Q, const void* K, const void
     p.k_bs = k_bs; p.k_rs = k_rs; p.k_hs = k_hs;
     p.v_bs = v_bs; p.v_rs = v_rs; p.v_hs = v_hs;
     p.o_bs = o_bs; p.o_rs = o_rs; p.o_hs = o_hs;
+    p.g_bs = g_bs; p.g_rs = g_rs; p.g_hs = g_hs;
     p.M = (int)M; p.N = (int)N;
     p.heads = (int)Hkv;
     p.G = (int)(Hq / Hkv);

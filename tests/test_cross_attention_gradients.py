@@ -19,16 +19,16 @@ U = {"f16": 2.0 ** -11, "bf16": 2.0 ** -8}
 
 def _backward(**over):
     a = dict(Q=FAKE, K=FAKE, V=FAKE, O=FAKE, dO=FAKE, lse=FAKE, lens=FAKE, dQ=FAKE, dK=FAKE, dV=FAKE, delta=FAKE, batch=2, M=5, N=7, Hq=4, Hkv=2, d=64, q=(1280, 256, 64), k=(896, 128, 64),
-             v=(896, 128, 64), o=(1280, 256, 64), scale=0.125, i="f16")
+             v=(896, 128, 64), o=(1280, 256, 64), go=(1280, 256, 64), scale=0.125, i="f16")
     a.update(over)
     return B.tir_cross_attention_backward_status(*[a[x] for x in ("Q", "K", "V", "O", "dO", "lse", "lens", "dQ", "dK", "dV", "delta", "batch", "M", "N", "Hq", "Hkv", "d")], *a["q"], *a["k"], *a["v"],
-                                                 *a["o"], a["scale"], a["i"])
+                                                 *a["o"], *a["go"], a["scale"], a["i"])
 
 
 @pytest.mark.parametrize("over,status", FAULTS + [
     (dict(dO=0), B.TIR_ERR_INVALID_ARG), (dict(lse=0), B.TIR_ERR_INVALID_ARG), (dict(dQ=0), B.TIR_ERR_INVALID_ARG), (dict(dK=0), B.TIR_ERR_INVALID_ARG), (dict(dV=0), B.TIR_ERR_INVALID_ARG),
     (dict(delta=0), B.TIR_ERR_INVALID_ARG), (dict(q=(0, 256, 64)), B.TIR_ERR_INVALID_ARG), (dict(q=(1280, 0, 64)), B.TIR_ERR_INVALID_ARG), (dict(k=(0, 128, 64)), B.TIR_ERR_INVALID_ARG),
-    (dict(v=(896, 0, 64)), B.TIR_ERR_INVALID_ARG), (dict(k=(896, 128, 0)), B.TIR_ERR_INVALID_ARG), (dict(dO=FAKE + 8), B.TIR_ERR_ALIGNMENT), (dict(dQ=FAKE + 8), B.TIR_ERR_ALIGNMENT),
+    (dict(v=(896, 0, 64)), B.TIR_ERR_INVALID_ARG), (dict(k=(896, 128, 0)), B.TIR_ERR_INVALID_ARG), (dict(go=(-8, 256, 64)), B.TIR_ERR_INVALID_ARG), (dict(go=(1280, 4, 64)), B.TIR_ERR_ALIGNMENT), (dict(dO=FAKE + 8), B.TIR_ERR_ALIGNMENT), (dict(dQ=FAKE + 8), B.TIR_ERR_ALIGNMENT),
     (dict(delta=FAKE + 2), B.TIR_ERR_ALIGNMENT), (dict(i="f32"), B.TIR_ERR_UNSUPPORTED)])
 def test_backward_rejects_bad_arguments(over, status):
     assert _backward(**over) == status and B.last_error()
@@ -43,16 +43,17 @@ def _forward_and_backward(q, kv, do, lens, scale, dtype, stream=None):
     import torch
     batch, m, hq, d = q.shape
     n, heads = kv.shape[1], kv.shape[3]
-    qd, kvd, dod = _to_device(q), _to_device(kv), do.cuda()
+    qd, kvd, dod = _to_device(q), _to_device(kv), _to_device(do)
     k, v = kvd[:, :, 0], kvd[:, :, 1]
-    o, lse, delta = torch.empty_like(dod), torch.empty((batch, hq, m), device="cuda"), torch.empty((batch, hq, m), device="cuda")
-    dq, dkv = torch.full_like(qd, MARK), torch.full_like(kvd, MARK)
+    o, lse, delta = torch.empty_like(qd), torch.empty((batch, hq, m), device="cuda"), torch.empty((batch, hq, m), device="cuda")
+    # (a gradient has the strides of what it is of, gaps included, which full_like would close)
+    dq, dkv = torch.empty_strided(qd.shape, qd.stride(), dtype=qd.dtype, device="cuda").fill_(MARK), torch.full_like(kvd, MARK)
     dk, dv = dkv[:, :, 0], dkv[:, :, 1]
     ld = None if lens is None else torch.tensor(lens, dtype=torch.int32, device="cuda")
     strides = (*qd.stride()[:3], *k.stride()[:3], *v.stride()[:3], *o.stride()[:3])
     torch.cuda.synchronize()
     B.tir_cross_attention(qd, k, v, o, lse, ld, batch, m, n, hq, heads, d, *strides, scale, dtype, dtype, stream)
-    B.tir_cross_attention_backward(qd, k, v, o, dod, lse, ld, dq, dk, dv, delta, batch, m, n, hq, heads, d, *strides, scale, dtype, stream)
+    B.tir_cross_attention_backward(qd, k, v, o, dod, lse, ld, dq, dk, dv, delta, batch, m, n, hq, heads, d, *strides, *dod.stride()[:3], scale, dtype, stream)
     torch.cuda.synchronize()
     return dict(dq=dq.cpu(), dk=dk.cpu(), dv=dv.cpu(), delta=delta.cpu())
 
@@ -214,6 +215,21 @@ def test_many_sequences_agree_with_one(workspace):
 
 
 @pytest.mark.gpu
+def test_gradients_that_arrive_in_other_orders(workspace):
+    """dO head by head, broadcast over the queries (the gradient of a sum), and as a slice; queries and keys as slices of wider tensors."""
+    import torch
+    for d in (64, 128):
+        g = _gen(19)
+        q, kv = _inputs(g, "f16", 2, 70, 90, 2, 2, d, [90, 31])
+        q = torch.randn((2, 70, 4, d + 24), generator=g).to(torch.float16)[..., 8:8 + d]
+        by_head = torch.randn((2, 4, 70, d), generator=g).to(torch.float16).transpose(1, 2)
+        one = torch.randn((2, 1, 4, d), generator=g).to(torch.float16).expand(2, 70, 4, d)
+        part = torch.randn((2, 70, 4, 2 * d), generator=g).to(torch.float16)[..., d:]
+        for do in (by_head, one, part):
+            _check(q, kv, do, [90, 31], 0.1, "f16", f"dO of strides {do.stride()}")
+
+
+@pytest.mark.gpu
 def test_no_queries_and_no_keys():
     import torch
     q, kv = _inputs(_gen(13), "f16", 2, 4, 6, 2, 1, 64, None)
@@ -244,7 +260,7 @@ def test_a_training_step_in_a_graph():
     with torch.cuda.graph(graph, stream=st, capture_error_mode="global"):
         B.tir_set_workspace(ws, st)
         B.tir_cross_attention(qd, k, v, o, lse, ld, batch, m, n, heads * group, heads, d, *strides, 0.125, "bf16", "bf16", st)
-        B.tir_cross_attention_backward(qd, k, v, o, dod, lse, ld, dq, dkv[:, :, 0], dkv[:, :, 1], delta, batch, m, n, heads * group, heads, d, *strides, 0.125, "bf16", st)
+        B.tir_cross_attention_backward(qd, k, v, o, dod, lse, ld, dq, dkv[:, :, 0], dkv[:, :, 1], delta, batch, m, n, heads * group, heads, d, *strides, *dod.stride()[:3], 0.125, "bf16", st)
     for i in range(4):
         q, kv = _inputs(g, "bf16", batch, m, n, heads, group, d, None)
         do = torch.randn(q.shape, generator=g).to(torch.bfloat16)
