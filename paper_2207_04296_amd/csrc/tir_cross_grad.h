@@ -52,7 +52,8 @@ template <int DH, int RB> struct GradTile {
         return (unsigned)(row * rs * 2 + (((lane & 7) ^ grad_swz(row)) << 4));
     }
     static __device__ __forceinline__ void copy(char* tile, const char* base, int left, int rs, unsigned off, int wave) {
-        const i32x4 r = make_rsrc(base, left > 0 ? (long long)(left - 1) * rs * 2 + ROW : 0);
+        const int rows = left < RB ? left : RB;
+        const i32x4 r = make_rsrc32(base, rows > 0 ? (unsigned)((rows - 1) * rs * 2 + ROW) : 0u);      // (rs of at most 2^23)
 #pragma unroll
         for (int h = 0; h < HALVES; ++h)
 #pragma unroll
@@ -155,6 +156,27 @@ template <int DT, int DB> __device__ __forceinline__ void round_ds(f32x16& ds, f
 constexpr float kFirstFactor = 0x1p100f;      // before any dS has been seen
 template <int DT> __device__ __forceinline__ float p_factor_log2() { return DT == DT_F16 ? 14.f : 0.f; }
 
+// The values are there at this point of the program: products are not moved behind what follows, where more of their operands would be held at a time.
+__device__ __forceinline__ void here(f32x16& x) { asm volatile("" : "+v"(x)); }
+
+struct TwoOperands {
+    uint4 a, b;
+};
+// N products with their operands read from LDS LA products ahead; nothing else moves between them, so that no more than LA operands are held.
+template <int N, int LA, class READ, class MUL> __device__ __forceinline__ void products(READ read, MUL mul) {
+    decltype(read(0)) f[LA];
+#pragma unroll
+    for (int t = 0; t < LA; ++t) f[t] = read(t);
+    TIR_FENCE();
+#pragma unroll
+    for (int t = 0; t < N; ++t) {
+        mul(t, f[t % LA]);
+        TIR_FENCE();
+        if (t + LA < N) f[t % LA] = read(t + LA);
+        TIR_FENCE();
+    }
+}
+
 // ---------------------------------------------------------------------------------------------
 // dQ: four waves of 32 rows (position, query head) each; keys and values through two LDS stages.
 // ---------------------------------------------------------------------------------------------
@@ -232,12 +254,13 @@ __global__ void __launch_bounds__(kGradThreads, 2) grad_rows_kernel(const GradPa
         const char* const tv = tk + T::BYTES;
 #pragma unroll
         for (int jb = 0; jb < kGradChunk / 32; ++jb) {
+            const int left = n - (c0 + i) * kGradChunk - jb * 32;      // keys of this block
+            if (left <= 0) break;
             f32x16 s, dp;
 #pragma unroll
             for (int ks = 0; ks < KSTEPS; ++ks) s = InTraits<DT>::mfma(T::along(tk, jb * 32, ks, l31, g), qf[ks], ks == 0 ? zero16 : s);
 #pragma unroll
             for (int ks = 0; ks < KSTEPS; ++ks) dp = InTraits<DT>::mfma(T::along(tv, jb * 32, ks, l31, g), of[ks], ks == 0 ? zero16 : dp);
-            const int left = n - (c0 + i) * kGradChunk - jb * 32;      // keys of this block
             f32x16 ds;
 #pragma unroll
             for (int r = 0; r < 16; ++r) ds[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], p.scale_log2e, -lse2)) * (dp[r] - delta);
@@ -278,14 +301,27 @@ __global__ void __launch_bounds__(kGradThreads, 2) grad_rows_kernel(const GradPa
 
 // ---------------------------------------------------------------------------------------------
 // dK and dV: four waves of 32 keys each; queries and dO, head after head, through two LDS stages with their lse and D.
+//
+// RG = 2: two groups of four waves on the same keys, which take every other chunk of rows through a ring each and are added through LDS at the end: two waves per SIMD where there is
+// one workgroup per CU.
+// A block's phases run one after the other (S and P, dV, dP and dS, dK): at d = 128 sums and keys are 160 registers, and 256 hold two waves per SIMD.  The values would be 32 more: there
+// they stay in LDS.
 // ---------------------------------------------------------------------------------------------
-template <int DT, int DH>
-__global__ void __launch_bounds__(kGradThreads, DH == 64 ? 2 : 1) grad_keys_kernel(const GradParams p) {
-    typedef GradTile<DH, kGradChunk> T;
-    constexpr int KSTEPS = DH / 16, DB = DH / 32, STAGE = 2 * T::BYTES + 2 * kGradChunk * 4;
-    __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
+template <int DT, int DH, int RG>
+__global__ void __launch_bounds__(kGradThreads * RG, 2) grad_keys_kernel(const GradParams p) {
+    constexpr int RB = DH == 64 ? 64 : 32;              // rows of a chunk
+    typedef GradTile<DH, RB> T;
+    constexpr int KSTEPS = DH / 16, DB = DH / 32, STAGE = 2 * T::BYTES + 2 * RB * 4, MERGE = 2 * DB * 4096;      // (MERGE: a wave's sums)
+    constexpr int LA = 3;
+    constexpr bool V_LDS = DH == 128;
+    typedef GradTile<DH, kGradTile> VT;
+    constexpr int V_AT = RG * 2 * STAGE, USED = V_AT + (V_LDS ? VT::BYTES : 0);
+    constexpr int LDS = USED > (RG - 1) * kGradWaves * MERGE ? USED : (RG - 1) * kGradWaves * MERGE;
+    __shared__ __attribute__((aligned(1024))) char smem[LDS];
     const int lane = threadIdx.x & 63, l31 = lane & 31, g = lane >> 5, blk = lane >> 4, s16 = lane & 15;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave_wg = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int rgrp = RG == 1 ? 0 : wave_wg / kGradWaves, wave = wave_wg - rgrp * kGradWaves;
+    char* const ring = smem + rgrp * 2 * STAGE;
     const int bh = (int)fastdiv(blockIdx.x, p.div_tiles_magic, p.div_tiles_shift);
     const int key0 = ((int)blockIdx.x - bh * p.tiles) * kGradTile;
     const int b = (int)fastdiv((unsigned)bh, p.div_h_magic, p.div_h_shift), h = bh - b * p.heads;
@@ -297,39 +333,56 @@ __global__ void __launch_bounds__(kGradThreads, DH == 64 ? 2 : 1) grad_keys_kern
     const int key = key0 + wave * 32 + l31;
     const bool live = key < n;
     // this slice's chunks of rows, of all query heads one after the other; none where the tile has no key
-    const int head_chunks = (p.M + kGradChunk - 1) / kGradChunk;
+    const int head_chunks = (p.M + RB - 1) / RB;
     const int all = key0 < n ? head_chunks * p.G : 0;
     const int per = (all + p.slices - 1) / p.slices;
     const int c0 = (int)blockIdx.y * per;
     const int chunks = all - c0 < per ? all - c0 : per;
+    const int mine = (chunks - rgrp + RG - 1) / RG;      // chunk i of this group is c0 + i * RG + rgrp
+    const int loops = (chunks + RG - 1) / RG;            // all groups take part in the barriers of the first
 
     const int q_rs = (int)p.q_rs, go_rs = (int)p.g_rs;
     const unsigned q_off = T::lane_offset(wave, lane, q_rs), go_off = T::lane_offset(wave, lane, go_rs);
-    int head_at = c0 / (head_chunks > 0 ? head_chunks : 1), chunk_at = c0 - head_at * head_chunks;      // of the next copy
-    auto copy = [&](int st_at) __attribute__((always_inline)) {
-        char* const st = smem + st_at * STAGE;
-        const int hq = h * p.G + head_at, m = chunk_at * kGradChunk, left = p.M - m;
-        T::copy(st, (const char*)p.Q + 2 * (b * p.q_bs + (long long)m * q_rs + hq * p.q_hs), left, q_rs, q_off, wave);
-        T::copy(st + T::BYTES, (const char*)p.dO + 2 * (b * p.g_bs + (long long)m * go_rs + hq * p.g_hs), left, go_rs, go_off, wave);
-        const long long stat = ((long long)b * p.heads * p.G + hq) * p.M + m;
-        if (wave < 2) floats_to_lds(make_rsrc((wave ? p.delta : p.lse) + stat, (long long)left * 4), st + 2 * T::BYTES + wave * (kGradChunk * 4), (unsigned)lane * 4);
-        if (++chunk_at == head_chunks) {
-            chunk_at = 0;
+    int head_at = 0, chunk_at = c0 + rgrp;               // of the next copy
+    auto settle = [&]() __attribute__((always_inline)) {
+        while (chunk_at >= head_chunks) {
+            chunk_at -= head_chunks;
             ++head_at;
         }
     };
-    if (chunks > 0) copy(0);
+    if (chunks > 0) {
+        head_at = chunk_at / head_chunks;
+        chunk_at -= head_at * head_chunks;
+    }
+    auto copy = [&](int st_at) __attribute__((always_inline)) {
+        char* const st = ring + st_at * STAGE;
+        const int hq = h * p.G + head_at, m = chunk_at * RB, left = p.M - m;
+        T::copy(st, (const char*)p.Q + 2 * (b * p.q_bs + (long long)m * q_rs + hq * p.q_hs), left, q_rs, q_off, wave);
+        T::copy(st + T::BYTES, (const char*)p.dO + 2 * (b * p.g_bs + (long long)m * go_rs + hq * p.g_hs), left, go_rs, go_off, wave);
+        const long long stat = ((long long)b * p.heads * p.G + hq) * p.M + m;
+        // (the lanes past RB floats would write past their place)
+        if (wave < 2 && lane < RB) floats_to_lds(make_rsrc32((wave ? p.delta : p.lse) + stat, (unsigned)(left < RB ? left : RB) * 4u), st + 2 * T::BYTES + wave * (RB * 4), (unsigned)lane * 4);
+        chunk_at += RG;
+        settle();
+    };
+    if (mine > 0) copy(0);
+    if (V_LDS && rgrp == 0 && chunks > 0)
+        VT::copy(smem + V_AT, (const char*)p.V + 2 * (b * p.v_bs + key0 * p.v_rs + h * p.v_hs), n - key0, (int)p.v_rs, VT::lane_offset(wave, lane, (int)p.v_rs), wave);
 
-    uint4 kf[KSTEPS], vf[KSTEPS];
+    uint4 kf[KSTEPS], vf[V_LDS ? 1 : KSTEPS];
 #pragma unroll
-    for (int ks = 0; ks < KSTEPS; ++ks) kf[ks] = vf[ks] = make_uint4(0, 0, 0, 0);
+    for (int ks = 0; ks < KSTEPS; ++ks) kf[ks] = make_uint4(0, 0, 0, 0);
+    if constexpr (!V_LDS)
+#pragma unroll
+        for (int ks = 0; ks < KSTEPS; ++ks) vf[ks] = make_uint4(0, 0, 0, 0);
     if (live) {
         const char* const k = (const char*)p.K + 2 * (b * p.k_bs + key * p.k_rs + h * p.k_hs) + g * 16;
-        const char* const v = (const char*)p.V + 2 * (b * p.v_bs + key * p.v_rs + h * p.v_hs) + g * 16;
 #pragma unroll
-        for (int ks = 0; ks < KSTEPS; ++ks) {
-            kf[ks] = *(const uint4*)(k + ks * 32);
-            vf[ks] = *(const uint4*)(v + ks * 32);
+        for (int ks = 0; ks < KSTEPS; ++ks) kf[ks] = *(const uint4*)(k + ks * 32);
+        if constexpr (!V_LDS) {
+            const char* const v = (const char*)p.V + 2 * (b * p.v_bs + key * p.v_rs + h * p.v_hs) + g * 16;
+#pragma unroll
+            for (int ks = 0; ks < KSTEPS; ++ks) vf[ks] = *(const uint4*)(v + ks * 32);
         }
     }
     f32x16 dk[DB], dv[DB];
@@ -341,60 +394,103 @@ __global__ void __launch_bounds__(kGradThreads, DH == 64 ? 2 : 1) grad_keys_kern
     const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-    for (int i = 0; i < chunks; ++i) {
+    for (int i = 0; i < loops; ++i) {
         copy_barrier<0>();
-        if (i + 1 < chunks) copy((i + 1) & 1);
-        const char* const tq = smem + (i & 1) * STAGE;
+        if (i + 1 < mine) copy((i + 1) & 1);
+        if (i >= mine) continue;               // (the longer group's last chunk)
+        const char* const tq = ring + (i & 1) * STAGE;
         const char* const to = tq + T::BYTES;
 #pragma unroll
-        for (int ib = 0; ib < kGradChunk / 32; ++ib) {
-            f32x16 s, dp;
-#pragma unroll
-            for (int ks = 0; ks < KSTEPS; ++ks) s = InTraits<DT>::mfma(T::along(tq, ib * 32, ks, l31, g), kf[ks], ks == 0 ? zero16 : s);
-#pragma unroll
-            for (int ks = 0; ks < KSTEPS; ++ks) dp = InTraits<DT>::mfma(T::along(to, ib * 32, ks, l31, g), vf[ks], ks == 0 ? zero16 : dp);
+        for (int ib = 0; ib < RB / 32; ++ib) {
+            f32x16 pr;
+            products<KSTEPS, LA>([&](int ks) __attribute__((always_inline)) { return T::along(tq, ib * 32, ks, l31, g); },
+                                 [&](int ks, const uint4& x) __attribute__((always_inline)) { pr = InTraits<DT>::mfma(x, kf[ks], ks == 0 ? zero16 : pr); });
             // row 8*a + 4*g + e of the block is register 4*a + e.  Rows behind the last read zeros: P = 1 there, dO and dS are 0.
-            unsigned pw[8], w[8];
-            f32x16 ds;
+            unsigned w[8];
 #pragma unroll
             for (int a = 0; a < 4; ++a) {
                 const f32x4 l4 = *(const f32x4*)(to + T::BYTES + (ib * 32 + 8 * a + 4 * g) * 4);
-                const f32x4 d4 = *(const f32x4*)(to + T::BYTES + kGradChunk * 4 + (ib * 32 + 8 * a + 4 * g) * 4);
-                float pr[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float t = __builtin_fmaf(s[4 * a + e], p.scale_log2e, l4[e] * -1.44269504088896340736f);
-                    pr[e] = __builtin_amdgcn_exp2f(t);
-                    ds[4 * a + e] = pr[e] * (dp[4 * a + e] - d4[e]);
-                    pr[e] = DT == DT_F16 ? pr[e] * 0x1p14f : pr[e];
-                }
-                pw[2 * a] = grad_pack<DT>(pr[0], pr[1]);
-                pw[2 * a + 1] = grad_pack<DT>(pr[2], pr[3]);
+                for (int e = 0; e < 4; ++e)
+                    pr[4 * a + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(pr[4 * a + e], p.scale_log2e, __builtin_fmaf(l4[e], -1.44269504088896340736f, p_factor_log2<DT>())));
+                w[2 * a] = grad_pack<DT>(pr[4 * a], pr[4 * a + 1]);
+                w[2 * a + 1] = grad_pack<DT>(pr[4 * a + 2], pr[4 * a + 3]);
             }
+            // dV of channel block t % DB from rows 16 * (t / DB) ..
+            products<2 * DB, LA>([&](int t) __attribute__((always_inline)) { return T::across(to, ib * 32 + t / DB * 16, t % DB, blk, s16); },
+                                 [&](int t, const uint4& x) __attribute__((always_inline)) {
+                                     const int ss = t / DB;
+                                     dv[t % DB] = InTraits<DT>::mfma(x, make_uint4(w[4 * ss], w[4 * ss + 1], w[4 * ss + 2], w[4 * ss + 3]), dv[t % DB]);
+                                 });
 #pragma unroll
-            for (int ss = 0; ss < 2; ++ss) {
-                const uint4 pf = make_uint4(pw[4 * ss], pw[4 * ss + 1], pw[4 * ss + 2], pw[4 * ss + 3]);
+            for (int db = 0; db < DB; ++db) here(dv[db]);
+            f32x16 ds;
+            if constexpr (V_LDS)
+                products<KSTEPS, LA>([&](int ks) __attribute__((always_inline)) { return TwoOperands{T::along(to, ib * 32, ks, l31, g), VT::along(smem + V_AT, wave * 32, ks, l31, g)}; },
+                                     [&](int ks, const TwoOperands& x) __attribute__((always_inline)) { ds = InTraits<DT>::mfma(x.a, x.b, ks == 0 ? zero16 : ds); });
+            else
+                products<KSTEPS, LA>([&](int ks) __attribute__((always_inline)) { return T::along(to, ib * 32, ks, l31, g); },
+                                     [&](int ks, const uint4& x) __attribute__((always_inline)) { ds = InTraits<DT>::mfma(x, vf[ks], ks == 0 ? zero16 : ds); });
 #pragma unroll
-                for (int db = 0; db < DB; ++db) dv[db] = InTraits<DT>::mfma(T::across(to, ib * 32 + ss * 16, db, blk, s16), pf, dv[db]);
+            for (int a = 0; a < 4; ++a) {
+                const f32x4 d4 = *(const f32x4*)(to + T::BYTES + RB * 4 + (ib * 32 + 8 * a + 4 * g) * 4);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) ds[4 * a + e] = pr[4 * a + e] * (ds[4 * a + e] - d4[e]);
             }
             round_ds<DT, DB>(ds, by, dk, w);
+            products<2 * DB, LA>([&](int t) __attribute__((always_inline)) { return T::across(tq, ib * 32 + t / DB * 16, t % DB, blk, s16); },
+                                 [&](int t, const uint4& x) __attribute__((always_inline)) {
+                                     const int ss = t / DB;
+                                     dk[t % DB] = InTraits<DT>::mfma(x, make_uint4(w[4 * ss], w[4 * ss + 1], w[4 * ss + 2], w[4 * ss + 3]), dk[t % DB]);
+                                 });
 #pragma unroll
-            for (int ss = 0; ss < 2; ++ss) {
-                const uint4 df = make_uint4(w[4 * ss], w[4 * ss + 1], w[4 * ss + 2], w[4 * ss + 3]);
-#pragma unroll
-                for (int db = 0; db < DB; ++db) dk[db] = InTraits<DT>::mfma(T::across(tq, ib * 32 + ss * 16, db, blk, s16), df, dk[db]);
-            }
+            for (int db = 0; db < DB; ++db) here(dk[db]);
         }
     }
-    const float fk = p.scale / by, fv = DT == DT_F16 ? 0x1p-14f : 1.f;
+    const float pf = DT == DT_F16 ? 0x1p-14f : 1.f;
+    const float fk = p.scale * pf / by, fv = pf;         // (dS was formed from probabilities times their factor)
+    if constexpr (RG > 1) {
+        __syncthreads();                                 // the rings are free
+        f32x4* const o = (f32x4*)(smem + wave * MERGE) + lane;
+        if (rgrp == 1) {
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int q4 = 0; q4 < 4; ++q4) {
+                    o[(db * 4 + q4) * 64] = f32x4{dk[db][4 * q4] * fk, dk[db][4 * q4 + 1] * fk, dk[db][4 * q4 + 2] * fk, dk[db][4 * q4 + 3] * fk};
+                    o[((DB + db) * 4 + q4) * 64] = f32x4{dv[db][4 * q4] * fv, dv[db][4 * q4 + 1] * fv, dv[db][4 * q4 + 2] * fv, dv[db][4 * q4 + 3] * fv};
+                }
+        }
+        __syncthreads();
+        if (rgrp == 1) return;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4) {
+                const f32x4 x = o[(db * 4 + q4) * 64], y = o[((DB + db) * 4 + q4) * 64];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    dk[db][4 * q4 + e] = __builtin_fmaf(dk[db][4 * q4 + e], fk, x[e]);
+                    dv[db][4 * q4 + e] = __builtin_fmaf(dv[db][4 * q4 + e], fv, y[e]);
+                }
+            }
+    } else {
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                dk[db][r] *= fk;
+                dv[db][r] *= fv;
+            }
+    }
     if (p.slices > 1) {
         f32x4* const o = (f32x4*)p.ws + ((long long)blockIdx.x * p.slices + blockIdx.y) * (2 * kGradTile * DH / 4) + wave * (32 * DH / 4) + lane;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
             for (int q4 = 0; q4 < 4; ++q4) {
-                o[(db * 4 + q4) * 64] = f32x4{dk[db][4 * q4] * fk, dk[db][4 * q4 + 1] * fk, dk[db][4 * q4 + 2] * fk, dk[db][4 * q4 + 3] * fk};
-                o[(db * 4 + q4) * 64 + kGradTile * DH / 4] = f32x4{dv[db][4 * q4] * fv, dv[db][4 * q4 + 1] * fv, dv[db][4 * q4 + 2] * fv, dv[db][4 * q4 + 3] * fv};
+                o[(db * 4 + q4) * 64] = f32x4{dk[db][4 * q4], dk[db][4 * q4 + 1], dk[db][4 * q4 + 2], dk[db][4 * q4 + 3]};
+                o[(db * 4 + q4) * 64 + kGradTile * DH / 4] = f32x4{dv[db][4 * q4], dv[db][4 * q4 + 1], dv[db][4 * q4 + 2], dv[db][4 * q4 + 3]};
             }
         return;
     }
@@ -406,8 +502,8 @@ __global__ void __launch_bounds__(kGradThreads, DH == 64 ? 2 : 1) grad_keys_kern
 #pragma unroll
         for (int q4 = 0; q4 < 4; ++q4) {
             const int at = db * 32 + q4 * 8 + 4 * g;
-            const uint2 x = make_uint2(grad_pack<DT>(dk[db][4 * q4] * fk, dk[db][4 * q4 + 1] * fk), grad_pack<DT>(dk[db][4 * q4 + 2] * fk, dk[db][4 * q4 + 3] * fk));
-            const uint2 y = make_uint2(grad_pack<DT>(dv[db][4 * q4] * fv, dv[db][4 * q4 + 1] * fv), grad_pack<DT>(dv[db][4 * q4 + 2] * fv, dv[db][4 * q4 + 3] * fv));
+            const uint2 x = make_uint2(grad_pack<DT>(dk[db][4 * q4], dk[db][4 * q4 + 1]), grad_pack<DT>(dk[db][4 * q4 + 2], dk[db][4 * q4 + 3]));
+            const uint2 y = make_uint2(grad_pack<DT>(dv[db][4 * q4], dv[db][4 * q4 + 1]), grad_pack<DT>(dv[db][4 * q4 + 2], dv[db][4 * q4 + 3]));
             *(uint2*)(ok + at) = live ? x : make_uint2(0, 0);
             *(uint2*)(ov + at) = live ? y : make_uint2(0, 0);
         }
@@ -422,6 +518,7 @@ template <int DT, int DH, bool KEYS> __global__ void __launch_bounds__(256) grad
     const int tile = (int)blockIdx.y, at = (int)(blockIdx.x * 256 + threadIdx.x);      // < PART: a multiple of 256
     const f32x4* const part = (const f32x4*)p.ws + (long long)tile * p.slices * PART + at;
     f32x4 sum = part[0];
+#pragma unroll 4
     for (int z = 1; z < p.slices; ++z) sum += part[(long long)z * PART];
     const int bh = (int)fastdiv((unsigned)tile, p.div_tiles_magic, p.div_tiles_shift);
     const int b = (int)fastdiv((unsigned)bh, p.div_h_magic, p.div_h_shift), h = bh - b * p.heads;

@@ -9,7 +9,11 @@ namespace tir {
 
 template <int DT, int DH, bool KEYS> static hipError_t launch_pass(const GradParams& p, hipStream_t stream) {
     const unsigned tiles = (unsigned)(p.batch * p.heads * p.tiles);
-    const hipError_t e = launch_kernel(KEYS ? &grad_keys_kernel<DT, DH> : &grad_rows_kernel<DT, DH>, dim3(tiles, (unsigned)p.slices), dim3(kGradThreads), stream, p);
+    const dim3 grid(tiles, (unsigned)p.slices);
+    hipError_t e;
+    if (!KEYS) e = launch_kernel(&grad_rows_kernel<DT, DH>, grid, dim3(kGradThreads), stream, p);
+    else if ((int64_t)tiles * p.slices <= 256) e = launch_kernel(&grad_keys_kernel<DT, DH, 2>, grid, dim3(2 * kGradThreads), stream, p);
+    else e = launch_kernel(&grad_keys_kernel<DT, DH, 1>, grid, dim3(kGradThreads), stream, p);
     if (e != hipSuccess || p.slices == 1) return e;
     return launch_kernel(&grad_sum_kernel<DT, DH, KEYS>, dim3((KEYS ? 2 : 1) * kGradTile * DH / 1024, tiles), dim3(256), stream, p);
 }
@@ -24,9 +28,9 @@ hipError_t launch_grad_rows(const GradParams& p, int dt, int dh, hipStream_t str
 hipError_t launch_grad_keys(const GradParams& p, int dt, int dh, hipStream_t stream) { return launch_by_type<true>(p, dt, dh, stream); }
 
 // How many workgroups share a tile's walk of `steps` chunks: as many as the chip has room for, each with two chunks at least, as far as the partial sums fit.
-static int slices_of(int64_t tiles, int64_t steps, int64_t part_bytes, const StreamWorkspace& ws) {
-    if (!ws.partial || tiles >= 256 || tiles > 65535) return 1;
-    int64_t s = 512 / tiles;
+static int slices_of(int64_t tiles, int64_t room, int64_t steps, int64_t part_bytes, const StreamWorkspace& ws) {
+    if (!ws.partial || tiles >= room) return 1;
+    int64_t s = room / tiles;
     if (s > steps / 2) s = steps / 2;
     if (s > ws.bytes / (tiles * part_bytes)) s = ws.bytes / (tiles * part_bytes);
     return s > 64 ? 64 : s < 2 ? 1 : (int)s;
@@ -89,12 +93,12 @@ tir_status tir_cross_attention_backward(const void* Q, const void* K, const void
         const FastDiv dt = make_fastdiv((unsigned)tiles);
         p.tiles = (int)tiles;
         p.div_tiles_magic = dt.magic; p.div_tiles_shift = dt.shift;
-        p.slices = slices_of(batch * Hkv * tiles, steps, kGradTile * d * 4 * (keys ? 2 : 1), ws);
+        p.slices = slices_of(batch * Hkv * tiles, keys ? 256 : 512, steps, kGradTile * d * 4 * (keys ? 2 : 1), ws);
         return keys ? launch_grad_keys(p, (int)in, (int)d, (hipStream_t)stream) : launch_grad_rows(p, (int)in, (int)d, (hipStream_t)stream);
     };
     hipError_t e = hipSuccess;
     if (M > 0) e = pass(false, (M * p.G + kGradTile - 1) / kGradTile, (N + kGradChunk - 1) / kGradChunk);
-    if (e == hipSuccess && N > 0) e = pass(true, (N + kGradTile - 1) / kGradTile, (M + kGradChunk - 1) / kGradChunk * p.G);
+    if (e == hipSuccess && N > 0) e = pass(true, (N + kGradTile - 1) / kGradTile, (M + 63) / 64 * p.G);
     if (e != hipSuccess) return host_error(TIR_ERR_LAUNCH, "%s: launch failed: %s", who, hipGetErrorString(e));
     return TIR_OK;
 }
