@@ -27,7 +27,7 @@ EXPORTS = ["tir_gemm", "tir_batch_matmul", "tir_conv2d", "tir_last_error", "tir_
            "tir_conv1d", "tir_conv3d", "tir_conv2d_transpose", "tir_debug_force_ksplit", "tir_debug_fastdiv",
            "tir_conv2d_transpose_variant", "tir_conv3d_variant", "tir_tune_conv3d", "tir_tune_conv2d_transpose",
            "tir_workspace_bytes", "tir_set_workspace", "tir_gemm_split_static", "tir_cache_append", "tir_cache_attention",
-           "tir_cross_attention", "tir_cross_attention_backward"]
+           "tir_cross_attention", "tir_cross_attention_backward", "tir_debug_cache_kernel"]
 
 
 class Epilogue(ctypes.Structure):
@@ -137,6 +137,8 @@ def lib() -> ctypes.CDLL:
     L.tir_debug_block_plan.restype = None
     L.tir_debug_attention_kernel.argtypes = [i64] * 4 + [ci]
     L.tir_debug_attention_kernel.restype = ctypes.c_char_p
+    L.tir_debug_cache_kernel.argtypes = [i64] * 7
+    L.tir_debug_cache_kernel.restype = ctypes.c_char_p
     L.tir_probe_mfma_rate.argtypes = [vp, ci, ci, ctypes.POINTER(ctypes.c_double), vp]
     L.tir_probe_mfma_rate.restype = ci
     L.tir_version.restype = ctypes.c_char_p
@@ -351,6 +353,10 @@ def tir_debug_block_plan() -> tuple[int, int]:
 
 def tir_debug_attention_kernel(batch: int, M: int, N: int, d: int, out_dtype) -> str:
     return lib().tir_debug_attention_kernel(batch, M, N, d, _code(out_dtype)).decode()
+
+
+def tir_debug_cache_kernel(batch: int, T: int, Hq: int, heads: int, d: int, block_tokens: int, columns: int) -> str:
+    return lib().tir_debug_cache_kernel(batch, T, Hq, heads, d, block_tokens, columns).decode()
 
 
 def tir_probe_mfma_rate(sink, iters: int, random_operands: bool, stream=None) -> float:

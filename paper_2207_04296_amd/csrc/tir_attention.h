@@ -120,7 +120,12 @@ __global__ void __launch_bounds__(QW * KG * 64, 2) attention_kernel(const P p) {
     // whose keys and values its L2 then holds once.
     const int nwg = p.batch * p.tiles_m;
     const int xq = nwg >> 3, xr = nwg & 7, xf = blockIdx.x & 7;
-    const int bid = xf * xq + (xf < xr ? xf : xr) + (blockIdx.x >> 3);
+    // Sequences of different lengths are dealt out instead, so that no domain gets the long ones alone.
+    const int bid = [&]() {
+        const int run = xf * xq + (xf < xr ? xf : xr) + (blockIdx.x >> 3);
+        if constexpr (std::is_same<P, CrossParams>::value) return p.lens ? (int)blockIdx.x : run;
+        else return run;
+    }();
     const long long b = fastdiv((unsigned)bid, p.div_tm_magic, p.div_tm_shift);
     const int tm = bid - (int)b * p.tiles_m;
     const int m0 = tm * TQ;

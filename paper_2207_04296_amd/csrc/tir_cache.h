@@ -40,6 +40,7 @@ struct CacheAttnParams {
     const int* count;       // its queries, at most T; null: T each
     int T, G;               // query heads per key head
     int batch, tiles;       // tiles of queries per sequence and key head
+    int rows_of_tile;       // which kernel: 32, or 32 * kCacheTileWaves
     int slices;             // workgroups that share a tile's keys
     int out32;              // fp32 output
     float scale_log2e;
@@ -48,6 +49,8 @@ struct CacheAttnParams {
     unsigned div_g_magic, div_h_magic, div_tiles_magic;      // / G, / heads, / tiles
     int div_g_shift, div_h_shift, div_tiles_shift;
 };
+
+constexpr int kCacheTileWaves = 8;
 
 hipError_t launch_append(const AppendParams& p, int dt, int ct, int d, int64_t batch, hipStream_t stream);
 hipError_t launch_cache_attention(const CacheAttnParams& p, int dt, int ct, int d, hipStream_t stream);
@@ -568,6 +571,404 @@ __global__ void __launch_bounds__(kCacheWaves * 64, 2) cache_rows_kernel(const C
         const f32x4 v = out[n] * inv;
         if (p.out32) *(f32x4*)((float*)p.O + at + ch) = v;
         else *(uint2*)((unsigned short*)p.O + at + ch) = make_uint2(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]));
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// The same for many rows: QW waves of 32 rows each over chunks of 64 keys, which the workgroup widens to 16 bits once, on their way from registers into LDS, instead of every wave
+// for itself (a wave that widens all it multiplies spends 160 instructions of a chunk's 400 on it).  K [64 keys][128 bytes] per 64 channels and V [channels][128 bytes of keys], both read along their
+// rows; 16-byte column c of row r at column c ^ swizzle(r), which spreads the 16 rows of a read phase over all banks: rows 0-3, 16-19, 4-7, 20-23 of K (the order above), 0-15 of V.
+//
+// A wave runs its vector work under its own products, as in the dense attention: the exponentials of chunk i and the widening of what comes next stand between the MFMAs of K Q^T of chunk i + 1, the row
+// maxima of that chunk between those of V^T P^T of chunk i.  Keys are therefore widened two chunks ahead of their weights and values one; what is widened was requested an iteration before, its block ids
+// one more.
+// ---------------------------------------------------------------------------------------------
+// How a tile's chunks are shared among workgroups: runs of at least four.
+struct TileShare {
+    int chunks, per, active;
+};
+__device__ __forceinline__ TileShare tile_share(int kmax, int slices) {
+    TileShare s;
+    s.chunks = (kmax + 63) >> 6;
+    s.per = (s.chunks + slices - 1) / slices;
+    s.per = slices > 1 && s.per < 4 ? 4 : s.per;
+    s.active = s.chunks > s.per ? (s.chunks + s.per - 1) / s.per : 1;
+    return s;
+}
+
+template <int DT, int CT, int DH, int QW>
+__global__ void __launch_bounds__(QW * 64, 2) cache_tile_kernel(const CacheAttnParams p) {
+    constexpr int NT = QW * 64, TQ = QW * 32, DB = DH / 32, KSTEPS = DH / 16;
+    constexpr int KBYTES = 64 * DH * 2, VBYTES = DH * 128;
+    constexpr int HALF_UNITS = 64 * DH / 16, U = 2 * HALF_UNITS / NT;      // 16-byte units of the keys or values of a chunk; units per thread
+    static_assert(U >= 1 && U * NT == 2 * HALF_UNITS, "");
+    __shared__ __attribute__((aligned(1024))) char smem[2 * KBYTES + 2 * VBYTES + 4 * 64];
+    char* const lds_v = smem + 2 * KBYTES;
+    char* const lds_s = lds_v + 2 * VBYTES;                                // four chunks' scales: {factor of the scores, log2(vs), 1 / vs} of each granule of 16 tokens
+    const int tid = (int)threadIdx.x, lane = tid & 63, l31 = lane & 31, g = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int bh = (int)fastdiv(blockIdx.x, p.div_tiles_magic, p.div_tiles_shift);
+    const int row0 = ((int)blockIdx.x - bh * p.tiles) * TQ;
+    const int b = (int)fastdiv((unsigned)bh, p.div_h_magic, p.div_h_shift);
+    const int h = bh - b * p.c.heads;
+    const int bt = 1 << p.c.shift;
+    const long long cap = (long long)p.c.cols << p.c.shift;
+    int len = p.lens[b], cnt = p.count ? p.count[b] : p.T;
+    len = len < 0 ? 0 : (len > (int)cap ? (int)cap : len);
+    cnt = cnt < 0 ? 0 : (cnt > p.T ? p.T : cnt);
+    const int rows = cnt * p.G - row0;
+    if (rows <= 0) return;
+    auto seen_by = [&](int row) __attribute__((always_inline)) -> int {      // keys that a row of the sequence sees
+        const long long n = (long long)len - cnt + (int)fastdiv((unsigned)row, p.div_g_magic, p.div_g_shift) + 1;
+        return n < 0 ? 0 : (int)n;
+    };
+    const int kmax = seen_by(row0 + (rows < TQ ? rows : TQ) - 1);            // of the tile
+    const TileShare share = tile_share(kmax, p.slices);
+    if ((int)blockIdx.y >= share.active) return;
+    const int c0 = (int)blockIdx.y * share.per;                              // this workgroup's chunks: c0 .. c1 - 1
+    const int c1 = c0 + share.per < share.chunks ? c0 + share.per : share.chunks;
+    const int row = row0 + wave * 32 + l31;
+    const bool live = wave * 32 + l31 < rows;
+    const int t_lane = (int)fastdiv((unsigned)row, p.div_g_magic, p.div_g_shift), g_lane = row - t_lane * p.G;
+    const int lim = live ? seen_by(row) : kmax;                              // (rows behind the last one take part and are dropped)
+    const int wmin = wave * 32 < rows ? seen_by(row0 + wave * 32) : kmax;    // from where on a chunk needs the wave's limits
+
+    // ------------------------------------------------------------ from the pool to LDS
+    // Unit u of this thread: 16 channels of a key (keys) or a channel's 16 keys (values).  Where a side has fewer units than threads, each half of the waves has one side.
+    const int* const table = p.c.table + (long long)b * p.c.cols;
+    auto is_key = [&](int u) __attribute__((always_inline)) -> bool { return HALF_UNITS >= NT ? u * NT < HALF_UNITS : wave < QW / 2; };
+    auto unit = [&](int u) __attribute__((always_inline)) -> int { return (tid + u * NT) & (HALF_UNITS - 1); };
+    auto granule = [&](int u) __attribute__((always_inline)) -> int { return is_key(u) ? unit(u) / KSTEPS >> 4 : unit(u) & 3; };
+    auto block_of = [&](int i, int gr) __attribute__((always_inline)) -> int {      // block of granule gr of chunk i, or -1
+        const int tok = i * 64 + gr * 16;            // (below 2^31: the table's columns end before)
+        return tok < kmax ? table[tok >> p.c.shift] : -1;
+    };
+    const unsigned block_bytes = (unsigned)(p.c.heads * DH) << p.c.shift;      // of one block in either pool: at most 65535 * 128 * 128
+    const char* const pool_k = p.c.k + ((unsigned)(h * DH) << p.c.shift);
+    const char* const pool_v = p.c.v + ((unsigned)(h * DH) << p.c.shift);
+    // the unit's place in a tile, less the tokens from the tile's start to the granule
+    unsigned off[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) off[u] = is_key(u) ? (unsigned)(unit(u) / KSTEPS % 16 * DH + unit(u) % KSTEPS * 16) : (unsigned)(unit(u) >> 2) << p.c.shift;
+    int ids[U], sid = -1, ok[U], sok = 0;
+    u32x4 w[U];
+    float ks = 0.f, vs = 0.f;
+    // keys and scales of chunk ck, values of chunk cv
+    auto fetch_ids = [&](int ck, int cv) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) ids[u] = block_of(is_key(u) ? ck : cv, granule(u));
+        if (tid < 4) sid = block_of(ck, tid);
+    };
+    auto fetch = [&](int ck, int cv) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            ok[u] = (unsigned)ids[u] < (unsigned)p.c.blocks;
+            const unsigned first = (unsigned)(((is_key(u) ? ck : cv) * 64 + granule(u) * 16) & (bt - 1));      // the granule's first token in its block
+            const unsigned long long at = (unsigned long long)(unsigned)(ok[u] ? ids[u] : 0) * block_bytes + (off[u] + (is_key(u) ? first * DH : first));
+            w[u] = *(const u32x4*)((is_key(u) ? pool_k : pool_v) + at);
+        }
+        if (tid < 4) {
+            sok = (unsigned)sid < (unsigned)p.c.blocks;
+            const long long base = (long long)(sok ? sid : 0) * p.c.heads + h;
+            ks = p.c.ks[base];
+            vs = p.c.vs[base];
+        }
+    };
+    const float sc = __builtin_fabsf(p.scale_log2e);      // (a negative scale is a positive one on negated queries)
+    auto swz_k = [](int r) __attribute__((always_inline)) { return ((r >> 1) & 3) | ((r >> 4) & 1) << 2; };
+    auto put_unit = [&](int u, int ck, int cv) __attribute__((always_inline)) {
+        const int q = unit(u);
+        u32x4 x = w[u];
+        if (is_key(u)) {
+            const int key = q / KSTEPS, c = q % KSTEPS;      // channels 16*c ..
+            // what lies behind the sequence is no value: zeros, whatever the bytes say
+            if (!ok[u] || ck * 64 + key >= len) x = u32x4{0, 0, 0, 0};
+            char* const at = smem + (ck & 1) * KBYTES + (c >> 2) * (64 * 128) + key * 128;
+            *(uint4*)(at + ((((c & 3) * 2) ^ swz_k(key)) << 4)) = widen_here<DT, CT>(x[0], x[1]);
+            *(uint4*)(at + ((((c & 3) * 2 + 1) ^ swz_k(key)) << 4)) = widen_here<DT, CT>(x[2], x[3]);
+        } else {
+            const int ch = q >> 2, gr = q & 3;
+            const int nv = ok[u] ? len - cv * 64 - gr * 16 : 0;
+            if (nv < 16) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int left = nv - 4 * e;
+                    x[e] &= left >= 4 ? ~0u : (left <= 0 ? 0u : (1u << (8 * left)) - 1u);
+                }
+            }
+            char* const at = lds_v + (cv & 1) * VBYTES + ch * 128;
+            *(uint4*)(at + (((gr * 2) ^ kmajor_swz<128>(ch)) << 4)) = widen_here<DT, CT>(x[0], x[1]);
+            *(uint4*)(at + (((gr * 2 + 1) ^ kmajor_swz<128>(ch)) << 4)) = widen_here<DT, CT>(x[2], x[3]);
+        }
+    };
+    auto put_scales = [&](int ck) __attribute__((always_inline)) {
+        if (tid < 4) {
+            const float v = __builtin_fmaxf(vs, 0x1p-100f);
+            f32x4 s4 = {sc * ks, __builtin_amdgcn_logf(v), __builtin_amdgcn_rcpf(v), 0.f};
+            if (!sok) s4 = f32x4{0.f, -__builtin_inff(), 1.f, 0.f};      // not there: no weight
+            *(f32x4*)(lds_s + (ck & 3) * 64 + tid * 16) = s4;
+        }
+    };
+    auto barrier = []() __attribute__((always_inline)) { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+
+    fetch_ids(c0, c0);
+    fetch(c0, c0);
+    uint4 qf[KSTEPS];
+    {
+        const unsigned flip = p.scale_log2e < 0.f ? 0x80008000u : 0u;
+        const char* const q = (const char*)p.Q + 2 * (b * p.q_bs + t_lane * p.q_rs + (long long)(h * p.G + g_lane) * p.q_hs);
+#pragma unroll
+        for (int k = 0; k < KSTEPS; ++k) {
+            qf[k] = live ? *(const uint4*)(q + k * 32 + g * 16) : make_uint4(0, 0, 0, 0);
+            qf[k] = make_uint4(qf[k].x ^ flip, qf[k].y ^ flip, qf[k].z ^ flip, qf[k].w ^ flip);
+        }
+    }
+    fetch_ids(c0 + 1, c0);
+#pragma unroll
+    for (int u = 0; u < U; ++u) put_unit(u, c0, c0);
+    put_scales(c0);
+    fetch(c0 + 1, c0);                               // (the values of the first chunk again, which are there: the same store twice)
+    fetch_ids(c0 + 2, c0 + 1);
+#pragma unroll
+    for (int u = 0; u < U; ++u) put_unit(u, c0 + 1, c0);
+    put_scales(c0 + 1);
+    fetch(c0 + 2, c0 + 1);
+    fetch_ids(c0 + 3, c0 + 2);
+
+    f32x16 acc[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[db][r] = 0.f;
+    float m_run = -__FLT_MAX__, l_run = 0.f;
+    const int krow = 16 * ((l31 >> 2) & 1) + 4 * (l31 >> 3) + (l31 & 3);
+    const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+
+    auto k_frag = [&](int i, int t) __attribute__((always_inline)) -> uint4 {      // product t of K Q^T: k-step t / 2, keys 32 * (t % 2) ..
+        const int k = t >> 1;
+        return *(const uint4*)(smem + (i & 1) * KBYTES + (k >> 2) * (64 * 128) + ((t & 1) * 32 + krow) * 128 + ((((k & 3) * 2 + g) ^ swz_k(krow)) << 4));
+    };
+    auto v_frag = [&](int i, int t) __attribute__((always_inline)) -> uint4 {      // product t of V^T P^T: keys of step t / DB, channels 32 * (t % DB) ..
+        const int jb = t / (2 * DB), ss = t / DB % 2;
+        return *(const uint4*)(lds_v + (i & 1) * VBYTES + (t % DB * 32 + l31) * 128 + (((jb * 4 + 2 * g + ss) ^ kmajor_swz<128>(l31)) << 4));
+    };
+    auto scales = [&](int i, int jb) __attribute__((always_inline)) -> f32x4 { return *(const f32x4*)(lds_s + (i & 3) * 64 + (jb * 2 + g) * 16); };
+    auto mask = [&](int i, f32x16 (&s)[2]) __attribute__((always_inline)) {
+        if (i * 64 + 64 > wmin) {
+#pragma unroll
+            for (int jb = 0; jb < 2; ++jb) {
+                const int n = lim - i * 64 - jb * 32 - 16 * g;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[jb][r] = r < n ? s[jb][r] : -__builtin_inff();
+            }
+        }
+    };
+    // The largest t = s * factor + log2(vs) of the row in a chunk, from the scores' maxima (a factor of zero times a masked score is NaN, which a maximum passes over).
+    auto raise = [&](int i, float m0, float m1) __attribute__((always_inline)) {
+        const f32x4 a = scales(i, 0), c = scales(i, 1);
+        float mx = __builtin_fmaxf(__builtin_fmaf(m0, a[0], a[1]), __builtin_fmaf(m1, c[0], c[1]));
+        mx = __builtin_fmaxf(half_max(mx), -__FLT_MAX__);
+        if (__builtin_amdgcn_ballot_w64(mx > m_run) != 0) {
+            const float m_new = __builtin_fmaxf(m_run, mx);
+            const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+            m_run = m_new;
+            l_run *= alpha;
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[db][r] *= alpha;
+        }
+    };
+
+    constexpr int NQK = 2 * KSTEPS, NPV = 4 * DB, EPM = 32 / NQK;      // products; exponentials per product of the first kind
+    constexpr int LAK = DH == 64 ? 4 : 2, LAV = DH == 64 ? 3 : 2;      // products by which an operand's read runs ahead
+    // Chunk i: its scores are in cur and m_run is its reference.
+    auto chunk_step = [&](int i, f32x16 (&cur)[2], f32x16 (&nxt)[2], auto last_flag) __attribute__((always_inline)) {
+        constexpr bool LAST = decltype(last_flag)::value;
+        const float ref = m_run - weight_bits<DT>();
+        float mul[2], base[2], inv_vs[2];
+#pragma unroll
+        for (int jb = 0; jb < 2; ++jb) {
+            const f32x4 s4 = scales(i, jb);
+            mul[jb] = s4[0];
+            base[jb] = s4[1] - ref;
+            inv_vs[jb] = s4[2];
+        }
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(__builtin_fabsf(m_run) <= 1024.f) || mul[0] == 0.f || mul[1] == 0.f) != 0, 0)) {
+#pragma clang fp contract(off)
+            // exponents in place of the scores: for references beyond 1024 the rounding of a reference alone would be seen, and a factor of zero leaves masked scores NaN
+#pragma unroll
+            for (int jb = 0; jb < 2; ++jb) {
+                const float lvs = scales(i, jb)[1];
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const float t = __builtin_fmaf(cur[jb][r], mul[jb], lvs) - ref;
+                    cur[jb][r] = cur[jb][r] == -__builtin_inff() ? cur[jb][r] : t;
+                }
+                mul[jb] = 1.f;
+                base[jb] = 0.f;
+            }
+        }
+        unsigned pw[16];
+        float lsum[2] = {0.f, 0.f};
+        uint4 kf[LAK], vf[LAV];
+        if constexpr (!LAST) {
+#pragma unroll
+            for (int t = 0; t < LAK; ++t) kf[t] = k_frag(i + 1, t);
+        }
+        TIR_FENCE();
+#pragma unroll
+        for (int t = 0; t < NQK; ++t) {
+            if constexpr (!LAST) {
+                nxt[t & 1] = InTraits<DT>::mfma(kf[t % LAK], qf[t >> 1], t < 2 ? zero16 : nxt[t & 1]);
+                TIR_FENCE();
+                if (t + LAK < NQK) kf[t % LAK] = k_frag(i + 1, t + LAK);
+                // keys of chunk i + 2 and values of chunk i + 1 to LDS, then the next ones on their way
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (t == 1 + u * (NQK - 4) / U) put_unit(u, i + 2, i + 1);
+                if (t == NQK - 4) put_scales(i + 2);
+                if (t == NQK - 3) fetch(i + 3, i + 2);
+                if (t == NQK - 2) fetch_ids(i + 4, i + 3);
+            }
+            if (t >= NQK - LAV) vf[t - (NQK - LAV)] = v_frag(i, t - (NQK - LAV));
+#pragma unroll
+            for (int e = t * EPM; e < (t + 1) * EPM; e += 2) {
+                const int jb = e / 16, r = e % 16;
+                float x[2];
+#pragma unroll
+                for (int z = 0; z < 2; ++z) {
+                    x[z] = __builtin_amdgcn_exp2f(__builtin_fmaf(cur[jb][r + z], mul[jb], base[jb]));
+                    lsum[jb] += x[z];
+                }
+                pw[e / 2] = pack2<DT>(x[0], x[1]);
+            }
+            TIR_FENCE();
+        }
+        l_run = __builtin_fmaf(lsum[0], inv_vs[0], __builtin_fmaf(lsum[1], inv_vs[1], l_run));
+        if constexpr (!LAST) mask(i + 1, nxt);
+        float mx[4];
+#pragma unroll
+        for (int t = 0; t < NPV; ++t) {
+            const int at = t / DB * 4;               // keys 16*(t / DB) .. of each half-wave's order: registers of pw
+            acc[t % DB] = InTraits<DT>::mfma(vf[t % LAV], make_uint4(pw[at], pw[at + 1], pw[at + 2], pw[at + 3]), acc[t % DB]);
+            TIR_FENCE();
+            if (t + LAV < NPV) vf[t % LAV] = v_frag(i, t + LAV);
+            if constexpr (!LAST) {
+                // the largest of chunk i + 1's scores, per granule, from the second product on: mx[jb], mx[2 + jb]
+                constexpr int PER = (32 + NPV - 2) / (NPV - 1);
+#pragma unroll
+                for (int e = (t - 1) * PER; t > 0 && e < t * PER && e < 32; ++e) {
+                    const int jb = e & 1, r = e >> 1, k = jb + 2 * (r & 1);
+                    mx[k] = r < 2 ? nxt[jb][r] : __builtin_fmaxf(mx[k], nxt[jb][r]);
+                }
+            }
+            TIR_FENCE();
+        }
+        if constexpr (!LAST) raise(i + 1, __builtin_fmaxf(mx[0], mx[2]), __builtin_fmaxf(mx[1], mx[3]));
+    };
+
+    f32x16 s_even[2], s_odd[2];
+    if (c0 < c1) {
+        barrier();
+#pragma unroll
+        for (int t = 0; t < NQK; ++t) s_even[t & 1] = InTraits<DT>::mfma(k_frag(c0, t), qf[t >> 1], t < 2 ? zero16 : s_even[t & 1]);
+        mask(c0, s_even);
+        float m[2];
+#pragma unroll
+        for (int jb = 0; jb < 2; ++jb) {
+            m[jb] = s_even[jb][0];
+#pragma unroll
+            for (int r = 1; r < 16; ++r) m[jb] = __builtin_fmaxf(m[jb], s_even[jb][r]);
+        }
+        raise(c0, m[0], m[1]);
+        barrier();                                   // (the first chunk's keys are overwritten from here on)
+        int i = c0;
+        for (; i + 2 < c1; i += 2) {
+            chunk_step(i, s_even, s_odd, std::false_type());
+            barrier();
+            chunk_step(i + 1, s_odd, s_even, std::false_type());
+            barrier();
+        }
+        if (i + 1 < c1) {
+            chunk_step(i, s_even, s_odd, std::false_type());
+            barrier();
+            ++i;
+#pragma unroll
+            for (int jb = 0; jb < 2; ++jb) s_even[jb] = s_odd[jb];
+        }
+        chunk_step(i, s_even, s_odd, std::true_type());
+    }
+    const float l = l_run + __shfl_xor(l_run, 32);
+    if (share.active > 1) {                          // partial results, joined by cache_join_kernel: [tile][slice][wave] as the other kernel's
+        char* const o = (char*)p.ws + (((long long)blockIdx.x * p.slices + blockIdx.y) * QW + wave) * cache_partial_bytes<DH>();
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4) ((f32x4*)o)[(db * 4 + q4) * 64 + lane] = f32x4{acc[db][4 * q4], acc[db][4 * q4 + 1], acc[db][4 * q4 + 2], acc[db][4 * q4 + 3]};
+        ((float*)(o + DB * 4096))[lane] = l;
+        ((float*)(o + DB * 4096))[64 + lane] = m_run;
+        return;
+    }
+    if (!live) return;
+    const float inv = lim > 0 && l != 0.f ? 1.0f / l : 0.f;
+    const long long at = b * p.o_bs + t_lane * p.o_rs + (long long)(h * p.G + g_lane) * p.o_hs;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+            const int ch = db * 32 + q4 * 8 + 4 * g;
+            const f32x4 v = {acc[db][4 * q4] * inv, acc[db][4 * q4 + 1] * inv, acc[db][4 * q4 + 2] * inv, acc[db][4 * q4 + 3] * inv};
+            if (p.out32) *(f32x4*)((float*)p.O + at + ch) = v;
+            else *(uint2*)((unsigned short*)p.O + at + ch) = make_uint2(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]));
+        }
+}
+
+// Joins the slices of cache_tile_kernel, in slice order: a workgroup per wave of a tile, one thread for a quarter of the channels of a row's half.
+template <int DT, int DH, int QW> __global__ void __launch_bounds__(256) cache_join_kernel(const CacheAttnParams p) {
+    constexpr int DB = DH / 32, PART = cache_partial_bytes<DH>();
+    const int tile = (int)blockIdx.x, wave = (int)blockIdx.y;
+    const int bh = (int)fastdiv((unsigned)tile, p.div_tiles_magic, p.div_tiles_shift);
+    const int row0 = (tile - bh * p.tiles) * (QW * 32);
+    const int b = (int)fastdiv((unsigned)bh, p.div_h_magic, p.div_h_shift), h = bh - b * p.c.heads;
+    const long long cap = (long long)p.c.cols << p.c.shift;
+    int len = p.lens[b], cnt = p.count ? p.count[b] : p.T;
+    len = len < 0 ? 0 : (len > (int)cap ? (int)cap : len);
+    cnt = cnt < 0 ? 0 : (cnt > p.T ? p.T : cnt);
+    const int rows = cnt * p.G - row0;
+    if (rows <= wave * 32) return;
+    const int last = row0 + (rows < QW * 32 ? rows : QW * 32) - 1;
+    const long long kmax = (long long)len - cnt + (int)fastdiv((unsigned)last, p.div_g_magic, p.div_g_shift) + 1;
+    const int active = tile_share(kmax < 0 ? 0 : (int)kmax, p.slices).active;
+    if (active == 1) return;
+    const int lane = (int)threadIdx.x & 63, l31 = lane & 31, g = lane >> 5, db = (int)threadIdx.x >> 6;
+    if (db >= DB) return;
+    const char* const part = (const char*)p.ws + ((long long)tile * p.slices * QW + wave) * PART;
+    auto slice = [&](int z) { return part + (long long)z * QW * PART; };
+    float top = -__FLT_MAX__, l = 0.f;
+#pragma unroll 4
+    for (int z = 0; z < active; ++z) top = __builtin_fmaxf(top, ((const float*)(slice(z) + DB * 4096))[64 + lane]);
+    f32x4 out[4];
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4) out[q4] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int z = 0; z < active; ++z) {
+        const float f = __builtin_amdgcn_exp2f(((const float*)(slice(z) + DB * 4096))[64 + lane] - top);
+        l += f * ((const float*)(slice(z) + DB * 4096))[lane];
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) out[q4] += f * ((const f32x4*)slice(z))[(db * 4 + q4) * 64 + lane];
+    }
+    if (wave * 32 + l31 >= rows) return;
+    const int row = row0 + wave * 32 + l31;
+    const int t = (int)fastdiv((unsigned)row, p.div_g_magic, p.div_g_shift);
+    const bool seen = (long long)len - cnt + t + 1 > 0;
+    const float inv = seen && l != 0.f ? 1.0f / l : 0.f;
+    const long long at = b * p.o_bs + t * p.o_rs + (long long)(h * p.G + row - t * p.G) * p.o_hs + db * 32 + 4 * g;
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4) {
+        const f32x4 v = out[q4] * inv;
+        if (p.out32) *(f32x4*)((float*)p.O + at + q4 * 8) = v;
+        else *(uint2*)((unsigned short*)p.O + at + q4 * 8) = make_uint2(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]));
     }
 }
 

@@ -1,5 +1,6 @@
 // Entry points of the paged cache and of attention over it: argument checks, choice of kernel, launch.
 #include <stdint.h>
+#include <stdio.h>
 
 #include "tir_host.h"
 #include "tir_launch.h"
@@ -19,7 +20,12 @@ hipError_t launch_append(const AppendParams& p, int dt, int ct, int d, int64_t b
 }
 
 template <int DT, int CT, int DH> static hipError_t launch_cache_as(const CacheAttnParams& p, hipStream_t stream) {
-    return launch_kernel(&cache_rows_kernel<DT, CT, DH>, dim3((unsigned)(p.batch * p.c.heads * p.tiles), (unsigned)p.slices), dim3(kCacheWaves * 64), stream, p);
+    const unsigned tiles = (unsigned)(p.batch * p.c.heads * p.tiles);
+    if (p.rows_of_tile == 32) return launch_kernel(&cache_rows_kernel<DT, CT, DH>, dim3(tiles, (unsigned)p.slices), dim3(kCacheWaves * 64), stream, p);
+    constexpr int QW = kCacheTileWaves;
+    const hipError_t e = launch_kernel(&cache_tile_kernel<DT, CT, DH, QW>, dim3(tiles, (unsigned)p.slices), dim3(QW * 64), stream, p);
+    if (e != hipSuccess || p.slices == 1) return e;
+    return launch_kernel(&cache_join_kernel<DT, DH, QW>, dim3(tiles, QW), dim3(256), stream, p);
 }
 hipError_t launch_cache_attention(const CacheAttnParams& p, int dt, int ct, int d, hipStream_t stream) {
 #define TIR_CACHE(DT, CT, DH) if (dt == DT && ct == CT && d == DH) return launch_cache_as<DT, CT, DH>(p, stream);
@@ -27,6 +33,46 @@ hipError_t launch_cache_attention(const CacheAttnParams& p, int dt, int ct, int 
     TIR_CACHE(DT_BF16, CT_I8, 64) TIR_CACHE(DT_BF16, CT_I8, 128) TIR_CACHE(DT_BF16, CT_E4M3, 64) TIR_CACHE(DT_BF16, CT_E4M3, 128)
 #undef TIR_CACHE
     return hipErrorInvalidValue;
+}
+
+// Tile of rows and number of workgroups that share a tile's keys.  How many keys a sequence holds is known on the device only: the table's columns bound it, and slices that
+// a short sequence does not need end at once.
+//
+// Tiles of 32 rows and of 256, us: 4 x 509 tokens x 32 query heads (8 key heads) of 128 over 4 thousand, e4m3 176 / 148, int8 and bf16 203 / 150, heads of 64 112 / 99; from fewer rows or workgroups the
+// small ones are as fast or faster: 1000 tokens over themselves 34.9 / 39.4, 64 x 20 tokens over 2500 139 / 187, 16 x 200 x 16 heads of 64 over 1200 42 / 56.
+static void choose_cache_kernel(CacheAttnParams* p, int64_t d, const StreamWorkspace& ws) {
+    const int64_t heads = (int64_t)p->batch * p->c.heads, rows = (int64_t)p->T * p->G, keys = (int64_t)p->c.cols << p->c.shift;
+    const int64_t part = d == 64 ? cache_partial_bytes<64>() : cache_partial_bytes<128>();
+    // tiles of 256 rows: one workgroup per CU, of which the tile's slices are to fill nearly all
+    const int64_t tall = heads * ((rows + 32 * kCacheTileWaves - 1) / (32 * kCacheTileWaves));
+    int64_t tall_slices = 1;
+    if (ws.partial && tall < 128) {
+        tall_slices = 256 / tall;
+        if (tall_slices > keys / 256) tall_slices = keys / 256;
+        if (tall_slices > ws.bytes / (tall * kCacheTileWaves * part)) tall_slices = ws.bytes / (tall * kCacheTileWaves * part);
+        if (tall_slices < 1) tall_slices = 1;
+    }
+    int64_t tiles = heads * ((rows + 31) / 32), slices = 1;
+    p->rows_of_tile = 32;
+    if (rows >= 512 && tall * tall_slices >= 192) {
+        p->rows_of_tile = 32 * kCacheTileWaves;
+        tiles = tall;
+        slices = tall_slices;
+    } else if (ws.partial && tiles <= ws.counters && tiles < 512) {
+        slices = (512 + tiles - 1) / tiles;
+        if (slices > (keys + 255) / 256) slices = (keys + 255) / 256;      // two chunks of 32 keys for each of a workgroup's four waves
+        if (slices > 64) slices = 64;
+        if (slices > ws.bytes / (tiles * part)) slices = ws.bytes / (tiles * part);
+        if (slices < 1) slices = 1;
+    }
+    p->tiles = (int)(tiles / heads);
+    p->slices = (int)slices;
+    if (slices > 1) {
+        p->ws = ws.partial;
+        p->ws_count = ws.count;
+    }
+    const FastDiv dt = make_fastdiv((unsigned)p->tiles);
+    p->div_tiles_magic = dt.magic; p->div_tiles_shift = dt.shift;
 }
 
 static tir_status check_cache(const char* who, const tir_kv_cache* c, int64_t batch, CacheView* out) {
@@ -118,39 +164,38 @@ tir_status tir_cache_attention(const void* Q, const tir_kv_cache* cache, void* O
     if (T > kMax31 || Hq > kMax31 || T > (kMax31 - 64) / (Hq / p.c.heads)) return host_error(TIR_ERR_UNSUPPORTED, "extent beyond 2^31-1");
     p.G = (int)(Hq / p.c.heads);
     p.T = (int)T;
-    const int64_t tiles = (T * p.G + 31) / 32;
-    if (batch > kMax31 / p.c.heads || batch * p.c.heads > kMax31 / tiles) return host_error(TIR_ERR_UNSUPPORTED, "%s: too many tiles of queries", who);
+    if (batch > kMax31 / p.c.heads || batch * p.c.heads > kMax31 / ((T * p.G + 31) / 32)) return host_error(TIR_ERR_UNSUPPORTED, "%s: too many tiles of queries", who);
     p.batch = (int)batch;
-    p.tiles = (int)tiles;
     p.Q = Q; p.O = O;
     p.q_bs = q_bs; p.q_rs = q_rs; p.q_hs = q_hs;
     p.o_bs = o_bs; p.o_rs = o_rs; p.o_hs = o_hs;
     p.lens = lens; p.count = count;
     p.out32 = out == TIR_F32;
     p.scale_log2e = scale * 1.44269504088896340736f;
-    const FastDiv dg = make_fastdiv((unsigned)p.G), dh = make_fastdiv((unsigned)p.c.heads), dt = make_fastdiv((unsigned)tiles);
+    const FastDiv dg = make_fastdiv((unsigned)p.G), dh = make_fastdiv((unsigned)p.c.heads);
     p.div_g_magic = dg.magic; p.div_g_shift = dg.shift;
     p.div_h_magic = dh.magic; p.div_h_shift = dh.shift;
-    p.div_tiles_magic = dt.magic; p.div_tiles_shift = dt.shift;
-    p.slices = 1;
-    const int64_t groups = batch * p.c.heads * tiles;
-    const StreamWorkspace ws = stream_workspace((hipStream_t)stream);
-    if (ws.partial && groups <= ws.counters && groups < 512) {
-        const int64_t part = cache->d == 64 ? cache_partial_bytes<64>() : cache_partial_bytes<128>();
-        int64_t slices = (512 + groups - 1) / groups;
-        const int64_t chunks = (((int64_t)p.c.cols << p.c.shift) + 31) / 32;
-        if (slices > (chunks + 7) / 8) slices = (chunks + 7) / 8;
-        if (slices > 64) slices = 64;
-        if (slices > ws.bytes / (groups * part)) slices = ws.bytes / (groups * part);
-        if (slices > 1) {
-            p.slices = (int)slices;
-            p.ws = ws.partial;
-            p.ws_count = ws.count;
-        }
-    }
+    choose_cache_kernel(&p, cache->d, stream_workspace((hipStream_t)stream));
     const hipError_t e = launch_cache_attention(p, (int)in, cache->dtype == TIR_I8 ? CT_I8 : CT_E4M3, (int)cache->d, (hipStream_t)stream);
     if (e != hipSuccess) return host_error(TIR_ERR_LAUNCH, "%s: launch failed: %s", who, hipGetErrorString(e));
     return TIR_OK;
+}
+
+const char* tir_debug_cache_kernel(int64_t batch, int64_t T, int64_t Hq, int64_t heads, int64_t d, int64_t block_tokens, int64_t columns) {
+    static thread_local char name[48];
+    CacheAttnParams p = {};
+    if (batch < 1 || T < 1 || heads < 1 || Hq < heads || columns < 1) return "";
+    p.batch = (int)batch;
+    p.T = (int)T;
+    p.G = (int)(Hq / heads);
+    p.c.heads = (int)heads;
+    p.c.cols = (int)columns;
+    while ((16ll << p.c.shift) < block_tokens * 16) ++p.c.shift;
+    // (a registered workspace, as the variant queries of the products assume one)
+    const StreamWorkspace ws = {(void*)256, nullptr, (int64_t)(tir_workspace_bytes() / (1 << 20)) << 20, 16384};
+    choose_cache_kernel(&p, d, ws);
+    snprintf(name, sizeof name, "rows%d/z%d", p.rows_of_tile, p.slices);
+    return name;
 }
 
 }  // extern "C"

@@ -17,6 +17,8 @@ template <int DT, int OUT, int DH, int QW, int KG, int KB, int FORM> static hipE
 }
 
 // The kernel by the rule for dense heads: a (sequence, key head) with the rows of all its query heads is a head of that rule, at the largest number of keys.
+// Sequences of different lengths leave the CUs of the short ones early: at d = 128 two workgroups of 128 rows per CU rather than one of 256, so that a long and a short one share a CU
+// (2 x 2047 x 4095 and 1365 keys x 16 heads of 128: 136 and 108 us; at d = 64, four or two per CU, 16 x 512 x 333 .. 1000 x 16 heads the same 45 us either way).
 template <int DT, int OUT, int DH> static hipError_t launch_cross(const CrossParams& p, hipStream_t stream) {
     const AttnKernel k = p.slices > 1 ? ATTN_T64_GROUPS : attention_kernel_of(p.batch, p.M, p.N, DH, OUT);
     if (k == ATTN_T64_GROUPS) return launch_cross_as<DT, OUT, DH, 2, 4, DH == 64 ? 64 : 32, ATTN_PIPED>(p, stream);
@@ -26,7 +28,7 @@ template <int DT, int OUT, int DH> static hipError_t launch_cross(const CrossPar
         if (k == ATTN_T128_SEQUENTIAL) return launch_cross_as<DT, OUT, DH, 4, 1, 64, ATTN_SEQUENTIAL>(p, stream);
         if (k == ATTN_T256_SEQUENTIAL) return launch_cross_as<DT, OUT, DH, 8, 1, 64, ATTN_SEQUENTIAL>(p, stream);
     } else {
-        if (k == ATTN_T256) return launch_cross_as<DT, OUT, DH, 8, 1, 64, ATTN_PIPED>(p, stream);
+        if (k == ATTN_T256 && !p.lens) return launch_cross_as<DT, OUT, DH, 8, 1, 64, ATTN_PIPED>(p, stream);
     }
     return launch_cross_as<DT, OUT, DH, 4, 1, 64, ATTN_PIPED>(p, stream);
 }

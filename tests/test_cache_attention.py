@@ -313,6 +313,61 @@ def test_cache_attention_matches_the_plain_form(workspace, cache, dtype, out, he
     _check_attention(pool, table, q, lens, count, d ** -0.5, dtype, out, what)
 
 
+# calls that take the tiles of 256 rows: many heads, and few over many keys, shared among workgroups
+TALL = [
+    (2, 32, 5, 64, 32, 131, [400, 131], [131, 120], "rows256/z1"),      # (batch, key heads, query heads per key head, d, block, T, lens, count, kernel)
+    (1, 64, 3, 128, 16, 180, [300], None, "rows256/z1"),
+    (2, 32, 4, 64, 128, 140, [130, 400], None, "rows256/z1"),           # the first sequence is shorter than its queries
+    (1, 4, 4, 64, 64, 130, [5001], None, "rows256/z20"),
+    (2, 2, 8, 128, 32, 70, [4500, 63], [70, 70], "rows256/z17"),
+    (3, 2, 8, 64, 16, 64, [4300, 4096, 200], [64, 1, 33], "rows256/z16"),
+]
+
+
+def test_the_tall_calls_take_the_tall_tiles():
+    for batch, heads, group, d, bt, T, lens, count, kernel in TALL:
+        assert B.tir_debug_cache_kernel(batch, T, heads * group, heads, d, bt, -(-max(lens) // bt) + 1) == kernel
+    assert B.tir_debug_cache_kernel(64, 1, 32, 8, 128, 64, 128) == "rows32/z1"
+    assert B.tir_debug_cache_kernel(1, 1, 32, 8, 128, 128, 1563) == "rows32/z64"
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("cache,dtype,out", [("i8", "f16", "f16"), ("e4m3", "f16", "f32"), ("i8", "bf16", "f32"), ("e4m3", "bf16", "bf16")])
+@pytest.mark.parametrize("shape", TALL)
+def test_cache_attention_of_many_rows(workspace, shape, cache, dtype, out):
+    import torch
+    batch, heads, group, d, bt, T, lens, count, kernel = shape
+    g = _gen(heads + T)
+    pool, table, q = _attention_case(g, cache, dtype, batch, T, heads, group, d, bt, lens)
+    what = f"cache attention {cache} {dtype}->{out} {shape}"
+    _say(what)
+    first = _check_attention(pool, table, q, lens, count, d ** -0.5, dtype, out, what)
+    again = _check_attention(pool, table, q, lens, count, d ** -0.5, dtype, out, what)
+    assert torch.equal(first, again)
+    table[0, 1] = -1                                         # a block that is not there, in the first chunk or the second
+    _check_attention(pool, table, q, lens, count, -0.3, dtype, out, what + ", a block missing, negative scale")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("cache,dtype", [("i8", "f16"), ("e4m3", "bf16")])
+@pytest.mark.parametrize("scale", [0.0, 3.0, 100.0])
+def test_many_rows_with_other_scales(workspace, cache, dtype, scale):
+    """Scale zero, scores of hundreds, and of thousands, where exponent and reference are rounded apart.  A score s = scale * q.k is a sum of 64 products in fp32, off by up to
+    16 * 2^-24 of their magnitudes' sum (the products' own order of summation: at most 16 additions deep), a probability by as much of itself, a row by twice that of T."""
+    import torch
+    batch, heads, group, d, bt, T, lens = 2, 32, 5, 64, 32, 131, [400, 131]
+    g = _gen(61)
+    pool, table, q = _attention_case(g, cache, dtype, batch, T, heads, group, d, bt, lens)
+    pool = list(pool)
+    pool[3] = pool[3] * torch.exp2(torch.randint(-12, 13, pool[3].shape, generator=g).float())
+    _say(f"many rows, {cache} {dtype}, scale {scale}")
+    _, got = _run_attention(pool, table, q, lens, None, scale, dtype, "f32")
+    ref, tt = R.cache_attention(q, *pool, table, lens, [T] * 2, scale)
+    largest = float((pool[0].float() * pool[2][..., None, None]).nan_to_num(0).abs().amax()) * float(q.float().abs().sum(-1).max())
+    tol = _tolerance(tt, ref, dtype, "f32") + 2 * scale * largest * 2.0 ** -20 * tt
+    assert torch.all((got.double() - ref).abs() <= tol)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("cache,dtype", [("i8", "f16"), ("e4m3", "bf16")])
 @pytest.mark.parametrize("scale", [0.0, -0.125, 3.0])
