@@ -489,8 +489,11 @@ __global__ void __launch_bounds__(kCacheWaves * 64, 2) cache_rows_kernel(const C
     }
 
     // ------------------------------------------------------------ the waves' results, relative to the largest reference
-    l_run += __shfl_xor(l_run, 32);
-    {
+    constexpr int NG = DB * 4 / KG;                      // groups of four channels this wave finishes
+    static_assert(NG * KG == DB * 4, "");
+    f32x4 out[NG];
+    float top, l;
+    auto join = [&]() __attribute__((always_inline)) {
         f32x4* const o = (f32x4*)(smem + wave * MERGE);
 #pragma unroll
         for (int db = 0; db < DB; ++db)
@@ -504,32 +507,33 @@ __global__ void __launch_bounds__(kCacheWaves * 64, 2) cache_rows_kernel(const C
         float* const t = (float*)(smem + wave * MERGE + DB * 4096);
         t[lane] = l_run;
         t[64 + lane] = m_run;
-    }
-    __syncthreads();
-    float top = -__FLT_MAX__, f[KG], l = 0.f;
+        __syncthreads();
+        float f[KG];
+        top = -__FLT_MAX__;
+        l = 0.f;
 #pragma unroll
-    for (int k = 0; k < KG; ++k) {
-        f[k] = ((const float*)(smem + k * MERGE + DB * 4096))[64 + lane];
-        top = __builtin_fmaxf(top, f[k]);
-    }
+        for (int k = 0; k < KG; ++k) {
+            f[k] = ((const float*)(smem + k * MERGE + DB * 4096))[64 + lane];
+            top = __builtin_fmaxf(top, f[k]);
+        }
 #pragma unroll
-    for (int k = 0; k < KG; ++k) {
-        f[k] = __builtin_amdgcn_exp2f(f[k] - top);
-        l += f[k] * ((const float*)(smem + k * MERGE + DB * 4096))[lane];
-    }
-    constexpr int NG = DB * 4 / KG;                      // groups of four channels this wave finishes
-    static_assert(NG * KG == DB * 4, "");
-    f32x4 out[NG];
+        for (int k = 0; k < KG; ++k) {
+            f[k] = __builtin_amdgcn_exp2f(f[k] - top);
+            l += f[k] * ((const float*)(smem + k * MERGE + DB * 4096))[lane];
+        }
 #pragma unroll
-    for (int n = 0; n < NG; ++n) {
-        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+        for (int n = 0; n < NG; ++n) {
+            f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int k = 0; k < KG; ++k) v += f[k] * ((const f32x4*)(smem + k * MERGE))[(wave * NG + n) * 64 + lane];
-        out[n] = v;
-    }
+            for (int k = 0; k < KG; ++k) v += f[k] * ((const f32x4*)(smem + k * MERGE))[(wave * NG + n) * 64 + lane];
+            out[n] = v;
+        }
+    };
+    l_run += __shfl_xor(l_run, 32);
+    join();
     if (active > 1) {
         // Slices of a tile: as for the split reduction of a product, the partial results go through memory at system scope, the last to
-        // arrive adds them in slice order.
+        // arrive adds them in an order of their own: each wave its share of the slices (one after the other a load's trip to memory per slice would be seen), then the waves.
         constexpr int kSystemScope = 17;
         const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc((char*)p.ws + (long long)tile * p.slices * MERGE, 0, p.slices * MERGE, 0x00020000);
 #pragma unroll
@@ -544,23 +548,56 @@ __global__ void __launch_bounds__(kCacheWaves * 64, 2) cache_rows_kernel(const C
         unsigned* const flag = (unsigned*)smem;
         if (threadIdx.x == 0) *flag = __hip_atomic_fetch_add(p.ws_count + tile, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
         __syncthreads();
-        if (*flag != (unsigned)active - 1u) return;
+        const bool last = *flag == (unsigned)active - 1u;
+        __syncthreads();                                 // (the flag's place is the first wave's again)
+        if (!last) return;
         if (threadIdx.x == 0) __hip_atomic_store(p.ws_count + tile, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
-        top = -__FLT_MAX__;
-        for (int s = 0; s < active; ++s)
-            top = __builtin_fmaxf(top, __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rw, DB * 4096 + 256 + lane * 4, s * MERGE, kSystemScope)));
-        l = 0.f;
+        const int at_l = DB * 4096 + lane * 4;
+        auto load_ref = [&](int z) __attribute__((always_inline)) -> float {      // of a slice behind the last one: no weight
+            const float m = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rw, z < active ? at_l + 256 : (int)kOutOfRange, z * MERGE, kSystemScope));
+            return z < active ? m : -__FLT_MAX__;
+        };
+        m_run = -__FLT_MAX__;
+        constexpr int Z = 8;
+        for (int z0 = wave; z0 < active; z0 += KG * Z) {
+            float m[Z];
 #pragma unroll
-        for (int n = 0; n < NG; ++n) out[n] = f32x4{0.f, 0.f, 0.f, 0.f};
-        for (int s = 0; s < active; ++s) {
-            const float ms = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rw, DB * 4096 + 256 + lane * 4, s * MERGE, kSystemScope));
-            const float ls = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rw, DB * 4096 + lane * 4, s * MERGE, kSystemScope));
-            const float fs = __builtin_amdgcn_exp2f(ms - top);
-            l += fs * ls;
+            for (int z = 0; z < Z; ++z) m[z] = load_ref(z0 + z * KG);
 #pragma unroll
-            for (int n = 0; n < NG; ++n)
-                out[n] += fs * __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, ((wave * NG + n) * 64 + lane) * 16, s * MERGE, kSystemScope));
+            for (int z = 0; z < Z; ++z) m_run = __builtin_fmaxf(m_run, m[z]);
         }
+        l_run = 0.f;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[db][r] = 0.f;
+        constexpr int W = 2;                             // slices on their way at a time
+        for (int z0 = wave; z0 < active; z0 += KG * W) {
+            float m[W], ls[W];
+            u32x4 v[W][DB * 4];
+#pragma unroll
+            for (int z = 0; z < W; ++z) {
+                const int at = z0 + z * KG;
+                m[z] = load_ref(at);
+                ls[z] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rw, at < active ? at_l : (int)kOutOfRange, at * MERGE, kSystemScope));
+#pragma unroll
+                for (int n = 0; n < DB * 4; ++n)
+                    v[z][n] = __builtin_amdgcn_raw_buffer_load_b128(rw, at < active ? (n * 64 + lane) * 16 : (int)kOutOfRange, at * MERGE, kSystemScope);
+            }
+#pragma unroll
+            for (int z = 0; z < W; ++z) {
+                const float f = z0 + z * KG < active ? __builtin_amdgcn_exp2f(m[z] - m_run) : 0.f;
+                l_run += f * ls[z];
+#pragma unroll
+                for (int n = 0; n < DB * 4; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const unsigned t = v[z][n][e];
+                        acc[n >> 2][(n & 3) * 4 + e] += f * __builtin_bit_cast(float, t);
+                    }
+            }
+        }
+        join();
     }
     if (!live) return;
     const float inv = lim > 0 && l != 0.f ? 1.0f / l : 0.f;           // a row that sees no key is zero
