@@ -424,8 +424,8 @@ int tir_debug_depthwise_rows(int64_t N, int64_t P, int64_t Q, int64_t C, tir_dty
 void tir_debug_block_plan(int* planned, int* strips);
 /* Name of the kernel tir_attention launches for these sizes, head dimension (64 or 128) and output type: its tile of queries and form. */
 const char* tir_debug_attention_kernel(int64_t batch, int64_t M, int64_t N, int64_t d, tir_dtype out);
-/* Rows of the tiles tir_cache_attention uses for these sizes, and into how many workgroups' slices a tile's keys may be cut on a stream with a workspace: "rows32/z<slices>" or
- * "rows256/z<slices>".  Valid until the calling thread's next call. */
+/* Rows of the tiles tir_cache_attention uses for these sizes, and into how many workgroups' slices a tile's keys may be cut on a stream with a workspace: "rows16/z<slices>", "rows32/..." or
+ * "rows256/...".  Valid until the calling thread's next call. */
 const char* tir_debug_cache_kernel(int64_t batch, int64_t T, int64_t Hq, int64_t heads, int64_t d, int64_t block_tokens, int64_t columns);
 
 /*

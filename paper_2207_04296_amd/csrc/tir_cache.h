@@ -40,7 +40,7 @@ struct CacheAttnParams {
     const int* count;       // its queries, at most T; null: T each
     int T, G;               // query heads per key head
     int batch, tiles;       // tiles of queries per sequence and key head
-    int rows_of_tile;       // which kernel: 32, or 32 * kCacheTileWaves
+    int rows_of_tile;       // which kernel: 16, 32, or 32 * kCacheTileWaves
     int slices;             // workgroups that share a tile's keys
     int out32;              // fp32 output
     float scale_log2e;
@@ -605,6 +605,295 @@ __global__ void __launch_bounds__(kCacheWaves * 64, 2) cache_rows_kernel(const C
 #pragma unroll
     for (int n = 0; n < NG; ++n) {
         const int grp = wave * NG + n, ch = grp / 4 * 32 + grp % 4 * 8 + 4 * g;
+        const f32x4 v = out[n] * inv;
+        if (p.out32) *(f32x4*)((float*)p.O + at + ch) = v;
+        else *(uint2*)((unsigned short*)p.O + at + ch) = make_uint2(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]));
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// The same for up to 16 rows of a key head, a token's query heads for instance, on 16x16x32 MFMAs: half the products and exponentials of the tile of 32, and chunks of 64 keys in the same registers.
+//
+// Lane l is query l & 15; its group q = l >> 4 holds the scores of the 16 keys from 16*q: tile j of four has row i as key 16*(i >> 2) + 4*j + (i & 3), and rows 4*q .. 4*q + 3 come out in
+// group q.  A load instruction takes 64 consecutive bytes of 16 rows, of keys or of values, where the tile of 32 takes 32 bytes of 32: one token over 200 003, blocks of 128 tokens, 110 us there.
+// ---------------------------------------------------------------------------------------------
+template <int DT> __device__ __forceinline__ f32x4 mfma16(const uint4& a, const uint4& b, f32x4 c) {
+    if constexpr (DT == DT_F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+// Partial results of a slice: accumulators [DH / 16][64] of four, sums and references [64].
+template <int DH> constexpr int token_partial_bytes() { return DH / 16 * 1024 + 512; }
+
+template <int DT, int CT, int DH>
+__global__ void __launch_bounds__(kCacheWaves * 64, 2) cache_token_kernel(const CacheAttnParams p) {
+    constexpr int KG = kCacheWaves, CB = DH / 16, KP = DH / 64;      // channel blocks of 16; 16-byte loads of a key per lane
+    constexpr int MERGE = token_partial_bytes<DH>();
+    __shared__ __attribute__((aligned(1024))) char smem[KG * MERGE];
+    const int lane = threadIdx.x & 63, l15 = lane & 15, grp = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int tile = (int)blockIdx.x, slice = (int)blockIdx.y;       // one tile per sequence and key head
+    const int b = (int)fastdiv((unsigned)tile, p.div_h_magic, p.div_h_shift);
+    const int h = tile - b * p.c.heads;
+    const int bt = 1 << p.c.shift;
+
+    const long long cap = (long long)p.c.cols << p.c.shift;
+    int len = p.lens[b], cnt = p.count ? p.count[b] : p.T;
+    len = len < 0 ? 0 : (len > (int)cap ? (int)cap : len);
+    cnt = cnt < 0 ? 0 : (cnt > p.T ? p.T : cnt);
+    if (cnt == 0) return;
+    const int t_lane = (int)fastdiv((unsigned)l15, p.div_g_magic, p.div_g_shift), g_lane = l15 - t_lane * p.G;
+    const bool live = l15 < cnt * p.G;
+    const int lim = live ? len - cnt + t_lane + 1 : 0;                // keys this lane's query sees, none if not above 0
+    const int kmax = len, kmin = len - cnt + 1;                       // of the last query, and of the first (may be negative)
+    const int nch = (kmax + 63) >> 6;
+    int per = (nch + p.slices - 1) / p.slices;
+    per = (per + KG - 1) / KG * KG;                                   // one chunk per wave at least
+    const int active = nch > per ? (nch + per - 1) / per : 1;
+    if (slice >= active) return;
+    const int c_end = (slice + 1) * per < nch ? (slice + 1) * per : nch;
+    const int c_first = slice * per + wave;
+    const int mine = c_end > c_first ? (c_end - c_first + KG - 1) / KG : 0;
+
+    const int* const table = p.c.table + (long long)b * p.c.cols;
+    // Block ids of this wave's next 16 chunks, one granule of 16 tokens per lane
+    auto fetch_ids = [&](int i0) __attribute__((always_inline)) -> int {
+        const int i = i0 + (lane >> 2), tok = (c_first + i * KG) * 64 + (lane & 3) * 16;
+        return i < mine && tok < len ? table[tok >> p.c.shift] : -1;
+    };
+    int ids = fetch_ids(0), ids_next = 0;
+
+    uint4 qf[2 * KP];
+    {
+        const char* const q = (const char*)p.Q + 2 * (b * p.q_bs + t_lane * p.q_rs + (long long)(h * p.G + g_lane) * p.q_hs);
+#pragma unroll
+        for (int ks = 0; ks < 2 * KP; ++ks)           // step 2*k + s takes channels 64*k + 16*grp + 8*s ..: the order of the keys' 16-byte loads
+            qf[ks] = live ? *(const uint4*)(q + ((ks >> 1) * 64 + grp * 16 + (ks & 1) * 8) * 2) : make_uint4(0, 0, 0, 0);
+    }
+    f32x4 acc[CB];
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) acc[cb] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m_run = -__FLT_MAX__, l_run = 0.f;
+
+    const unsigned block_bytes = (unsigned)(p.c.heads * DH) << p.c.shift;
+    const char* const pool_k = p.c.k + ((unsigned)(h * DH) << p.c.shift);
+    const char* const pool_v = p.c.v + ((unsigned)(h * DH) << p.c.shift);
+    struct Chunk {
+        u32x4 k[4][KP], v[CB];
+        float ks, vs;
+        int bad;                    // this group's granule has no block
+    };
+    auto load = [&](int i, Chunk& c) __attribute__((always_inline)) {
+        const int at = (i & 15) * 4, tok = (c_first + i * KG) * 64;
+        const int idk = __shfl(ids, at + (l15 >> 2)), idv = __shfl(ids, at + grp);
+        const bool okk = (unsigned)idk < (unsigned)p.c.blocks, okv = (unsigned)idv < (unsigned)p.c.blocks;
+        const char* const kp = pool_k + (unsigned long long)(unsigned)(okk ? idk : 0) * block_bytes + (unsigned)(((tok + (l15 >> 2) * 16) & (bt - 1)) * DH + (l15 & 3) * DH + grp * 16);
+        const char* const vp = pool_v + (unsigned long long)(unsigned)(okv ? idv : 0) * block_bytes + (unsigned)(((tok + grp * 16) & (bt - 1)) + (l15 << p.c.shift));
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int k = 0; k < KP; ++k) c.k[j][k] = *(const u32x4*)(kp + j * 4 * DH + k * 64);
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+            c.v[cb] = *(const u32x4*)(vp + ((cb * 16) << p.c.shift));
+            TIR_FENCE();                      // (an address at a time)
+        }
+        const long long s = (long long)(okv ? idv : 0) * p.c.heads + h;
+        c.ks = p.c.ks[s];
+        c.vs = p.c.vs[s];
+        c.bad = !okv;
+    };
+    auto over_groups = [](float x) __attribute__((always_inline)) -> float {
+        const auto a = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+        const unsigned lo = a[0], hi = a[1];
+        return half_max(__builtin_fmaxf(__builtin_bit_cast(float, lo), __builtin_bit_cast(float, hi)));
+    };
+    auto step = [&](int i, Chunk& c) __attribute__((always_inline)) {
+        const int base = (c_first + i * KG) * 64 + grp * 16;      // of this group's keys
+        f32x4 s[4];
+#pragma unroll
+        for (int ks = 0; ks < 2 * KP; ++ks)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const u32x4 w = c.k[j][ks >> 1];
+                const uint4 kf = (ks & 1) ? widen_here<DT, CT>(w[2], w[3]) : widen_here<DT, CT>(w[0], w[1]);
+                s[j] = mfma16<DT>(kf, qf[ks], ks == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[j]);
+                TIR_FENCE();
+            }
+        const float vs = __builtin_fmaxf(c.vs, 0x1p-100f);
+        const float mul = p.scale_log2e * c.ks, lvs = __builtin_amdgcn_logf(vs);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[j][r] = __builtin_fmaf(s[j][r], mul, lvs);
+        if (base - grp * 16 + 64 > kmin || __builtin_amdgcn_ballot_w64(c.bad) != 0) {
+            const int n = c.bad ? 0 : lim - base;                 // keys of the lane's sixteen that its query sees (may be negative)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[j][r] = 4 * j + r < n ? s[j][r] : -__builtin_inff();
+            if constexpr (CT == CT_E4M3) {                        // (as in the tile of 32: NaN bytes behind the sequence)
+                const int nv = c.bad ? 0 : len - base;
+                u32x4 keep;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int left = nv - 4 * e;
+                    keep[e] = left >= 4 ? ~0u : (left <= 0 ? 0u : (1u << (8 * left)) - 1u);
+                }
+#pragma unroll
+                for (int cb = 0; cb < CB; ++cb) c.v[cb] = c.v[cb] & keep;
+            }
+        }
+        float mx = s[0][0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) mx = __builtin_fmaxf(mx, s[e >> 2][e & 3]);
+        mx = __builtin_fmaxf(over_groups(mx), -__FLT_MAX__);
+        if (__builtin_amdgcn_ballot_w64(mx > m_run) != 0) {
+            const float m_new = __builtin_fmaxf(m_run, mx);
+            const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+            m_run = m_new;
+            l_run *= alpha;
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[cb][r] *= alpha;
+        }
+        const float ref = m_run - weight_bits<DT>();
+        float sum[2] = {0.f, 0.f};
+        unsigned pw[8];
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+            float w[2];
+#pragma unroll
+            for (int z = 0; z < 2; ++z) {
+                w[z] = __builtin_amdgcn_exp2f(s[e >> 2][(e & 3) + z] - ref);
+                sum[z] += w[z];
+            }
+            pw[e / 2] = pack2<DT>(w[0], w[1]);
+        }
+        l_run += (sum[0] + sum[1]) * __builtin_amdgcn_rcpf(vs);
+#pragma unroll
+        for (int ss = 0; ss < 2; ++ss) {              // keys 16*grp + 8*ss ..
+            const uint4 pf = make_uint4(pw[4 * ss], pw[4 * ss + 1], pw[4 * ss + 2], pw[4 * ss + 3]);
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb) {
+                acc[cb] = mfma16<DT>(widen_here<DT, CT>(c.v[cb][2 * ss], c.v[cb][2 * ss + 1]), pf, acc[cb]);
+                TIR_FENCE();
+            }
+        }
+    };
+    Chunk even, odd;
+    // (behind the last chunk there is no block, and a load takes the pool's first: without a branch around the loads the two chunks need no copies)
+    load(0, even);
+    for (int i = 0; i < mine; i += 2) {
+        if ((i & 15) == 0) ids_next = fetch_ids(i + 16);
+        load(i + 1, odd);
+        step(i, even);
+        if (((i + 2) & 15) == 0) ids = ids_next;
+        load(i + 2, even);
+        if (i + 1 < mine) step(i + 1, odd);
+    }
+
+    // ------------------------------------------------------------ the waves' results, and the slices', as in the tile of 32
+    constexpr int NG = CB / KG;                       // channel blocks this wave finishes
+    static_assert(NG * KG == CB, "");
+    f32x4 out[NG];
+    float top, l;
+    auto join = [&]() __attribute__((always_inline)) {
+        f32x4* const o = (f32x4*)(smem + wave * MERGE);
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) o[cb * 64 + lane] = acc[cb];
+        float* const t = (float*)(smem + wave * MERGE + CB * 1024);
+        t[lane] = l_run;
+        t[64 + lane] = m_run;
+        __syncthreads();
+        float f[KG];
+        top = -__FLT_MAX__;
+        l = 0.f;
+#pragma unroll
+        for (int k = 0; k < KG; ++k) {
+            f[k] = ((const float*)(smem + k * MERGE + CB * 1024))[64 + lane];
+            top = __builtin_fmaxf(top, f[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < KG; ++k) {
+            f[k] = __builtin_amdgcn_exp2f(f[k] - top);
+            l += f[k] * ((const float*)(smem + k * MERGE + CB * 1024))[lane];
+        }
+#pragma unroll
+        for (int n = 0; n < NG; ++n) {
+            f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < KG; ++k) v += f[k] * ((const f32x4*)(smem + k * MERGE))[(wave * NG + n) * 64 + lane];
+            out[n] = v;
+        }
+    };
+    l_run += __shfl_xor(l_run, 16);
+    l_run += __shfl_xor(l_run, 32);
+    join();
+    if (active > 1) {
+        constexpr int kSystemScope = 17;
+        const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc((char*)p.ws + (long long)tile * p.slices * MERGE, 0, p.slices * MERGE, 0x00020000);
+#pragma unroll
+        for (int n = 0; n < NG; ++n)
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, out[n]), rw, ((wave * NG + n) * 64 + lane) * 16, slice * MERGE, kSystemScope);
+        if (wave == 0) {
+            __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, l), rw, CB * 1024 + lane * 4, slice * MERGE, kSystemScope);
+            __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, top), rw, CB * 1024 + 256 + lane * 4, slice * MERGE, kSystemScope);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        unsigned* const flag = (unsigned*)smem;
+        if (threadIdx.x == 0) *flag = __hip_atomic_fetch_add(p.ws_count + tile, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+        __syncthreads();
+        const bool last = *flag == (unsigned)active - 1u;
+        __syncthreads();
+        if (!last) return;
+        if (threadIdx.x == 0) __hip_atomic_store(p.ws_count + tile, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+        const int at_l = CB * 1024 + lane * 4;
+        auto load_ref = [&](int z) __attribute__((always_inline)) -> float {
+            const float m = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rw, z < active ? at_l + 256 : (int)kOutOfRange, z * MERGE, kSystemScope));
+            return z < active ? m : -__FLT_MAX__;
+        };
+        m_run = -__FLT_MAX__;
+        constexpr int Z = 8;
+        for (int z0 = wave; z0 < active; z0 += KG * Z) {
+            float m[Z];
+#pragma unroll
+            for (int z = 0; z < Z; ++z) m[z] = load_ref(z0 + z * KG);
+#pragma unroll
+            for (int z = 0; z < Z; ++z) m_run = __builtin_fmaxf(m_run, m[z]);
+        }
+        l_run = 0.f;
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) acc[cb] = f32x4{0.f, 0.f, 0.f, 0.f};
+        constexpr int W = 2;                          // slices on their way at a time
+        for (int z0 = wave; z0 < active; z0 += KG * W) {
+            float m[W], ls[W];
+            u32x4 v[W][CB];
+#pragma unroll
+            for (int z = 0; z < W; ++z) {
+                const int at = z0 + z * KG;
+                m[z] = load_ref(at);
+                ls[z] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rw, at < active ? at_l : (int)kOutOfRange, at * MERGE, kSystemScope));
+#pragma unroll
+                for (int cb = 0; cb < CB; ++cb) v[z][cb] = __builtin_amdgcn_raw_buffer_load_b128(rw, at < active ? (cb * 64 + lane) * 16 : (int)kOutOfRange, at * MERGE, kSystemScope);
+            }
+#pragma unroll
+            for (int z = 0; z < W; ++z) {
+                const float f = z0 + z * KG < active ? __builtin_amdgcn_exp2f(m[z] - m_run) : 0.f;
+                l_run += f * ls[z];
+#pragma unroll
+                for (int cb = 0; cb < CB; ++cb) acc[cb] += f * __builtin_bit_cast(f32x4, v[z][cb]);
+            }
+        }
+        join();
+    }
+    if (!live) return;
+    const float inv = lim > 0 && l != 0.f ? 1.0f / l : 0.f;           // a row that sees no key is zero
+    const long long at = b * p.o_bs + t_lane * p.o_rs + (long long)(h * p.G + g_lane) * p.o_hs;
+#pragma unroll
+    for (int n = 0; n < NG; ++n) {
+        const int ch = (wave * NG + n) * 16 + 4 * grp;
         const f32x4 v = out[n] * inv;
         if (p.out32) *(f32x4*)((float*)p.O + at + ch) = v;
         else *(uint2*)((unsigned short*)p.O + at + ch) = make_uint2(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]));

@@ -21,6 +21,7 @@ hipError_t launch_append(const AppendParams& p, int dt, int ct, int d, int64_t b
 
 template <int DT, int CT, int DH> static hipError_t launch_cache_as(const CacheAttnParams& p, hipStream_t stream) {
     const unsigned tiles = (unsigned)(p.batch * p.c.heads * p.tiles);
+    if (p.rows_of_tile == 16) return launch_kernel(&cache_token_kernel<DT, CT, DH>, dim3(tiles, (unsigned)p.slices), dim3(kCacheWaves * 64), stream, p);
     if (p.rows_of_tile == 32) return launch_kernel(&cache_rows_kernel<DT, CT, DH>, dim3(tiles, (unsigned)p.slices), dim3(kCacheWaves * 64), stream, p);
     constexpr int QW = kCacheTileWaves;
     const hipError_t e = launch_kernel(&cache_tile_kernel<DT, CT, DH, QW>, dim3(tiles, (unsigned)p.slices), dim3(QW * 64), stream, p);
@@ -53,16 +54,18 @@ static void choose_cache_kernel(CacheAttnParams* p, int64_t d, const StreamWorks
         if (tall_slices < 1) tall_slices = 1;
     }
     int64_t tiles = heads * ((rows + 31) / 32), slices = 1;
-    p->rows_of_tile = 32;
+    p->rows_of_tile = rows <= 16 ? 16 : 32;
     if (rows >= 512 && tall * tall_slices >= 192) {
         p->rows_of_tile = 32 * kCacheTileWaves;
         tiles = tall;
         slices = tall_slices;
     } else if (ws.partial && tiles <= ws.counters && tiles < 512) {
+        // four waves with two chunks of 32 keys each, or one of 64
+        const int64_t small = p->rows_of_tile == 32 ? part : d == 64 ? token_partial_bytes<64>() : token_partial_bytes<128>();
         slices = (512 + tiles - 1) / tiles;
-        if (slices > (keys + 255) / 256) slices = (keys + 255) / 256;      // two chunks of 32 keys for each of a workgroup's four waves
+        if (slices > (keys + 255) / 256) slices = (keys + 255) / 256;
         if (slices > 64) slices = 64;
-        if (slices > ws.bytes / (tiles * part)) slices = ws.bytes / (tiles * part);
+        if (slices > ws.bytes / (tiles * small)) slices = ws.bytes / (tiles * small);
         if (slices < 1) slices = 1;
     }
     p->tiles = (int)(tiles / heads);

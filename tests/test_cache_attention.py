@@ -300,6 +300,8 @@ def workspace():
     (1, 4, 128, 16, 1, [1, 31, 32, 129, 0, 1000], [1, 1, 0, 1, 1, 1]),
     (2, 3, 64, 32, 3, [3, 1, 100, 64, 0], [3, 3, 2, 1, 3]),            # more queries than tokens: the first see nothing
     (1, 8, 128, 32, 5, [5, 260, 97], None),
+    (2, 2, 64, 64, 8, [8, 200, 63, 3], [8, 5, 1, 7]),                  # sixteen rows, some of which see nothing
+    (1, 16, 128, 128, 1, [129, 1, 0, 640], None), (3, 5, 128, 16, 3, [3, 64, 65, 1000], [3, 3, 2, 3]),
     (3, 1, 128, 64, 40, [40, 333, 65, 17], [40, 40, 1, 17]),
     (1, 2, 64, 64, 150, [150, 700], [150, 133]),
     (2, 5, 64, 128, 31, [31, 129, 500], None),
@@ -327,8 +329,9 @@ TALL = [
 def test_the_tall_calls_take_the_tall_tiles():
     for batch, heads, group, d, bt, T, lens, count, kernel in TALL:
         assert B.tir_debug_cache_kernel(batch, T, heads * group, heads, d, bt, -(-max(lens) // bt) + 1) == kernel
-    assert B.tir_debug_cache_kernel(64, 1, 32, 8, 128, 64, 128) == "rows32/z1"
-    assert B.tir_debug_cache_kernel(1, 1, 32, 8, 128, 128, 1563) == "rows32/z64"
+    assert B.tir_debug_cache_kernel(64, 1, 32, 8, 128, 64, 128) == "rows16/z1"
+    assert B.tir_debug_cache_kernel(1, 1, 32, 8, 128, 128, 1563) == "rows16/z64"
+    assert B.tir_debug_cache_kernel(2, 5, 16, 4, 64, 16, 100) == "rows32/z7" and B.tir_debug_cache_kernel(2, 4, 16, 4, 64, 16, 100) == "rows16/z7"
 
 
 @pytest.mark.gpu
@@ -436,15 +439,16 @@ def test_cache_attention_of_clamped_lengths(workspace, cache, dtype):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("cache,dtype,d,bt", [("i8", "f16", 128, 64), ("e4m3", "bf16", 64, 16), ("i8", "bf16", 128, 128)])
-def test_cache_attention_shared_among_workgroups(cache, dtype, d, bt):
+@pytest.mark.parametrize("T", [1, 6])
+def test_cache_attention_shared_among_workgroups(cache, dtype, d, bt, T):
     """Few queries over many keys with and without a workspace, and the same call again: the same bits again, within the tolerance of each other."""
     import torch
     lens = [9001, 130, 5003, 0, 1]
-    pool, table, q = _attention_case(_gen(31), cache, dtype, 5, 1, 2, 4, d, bt, lens)
+    pool, table, q = _attention_case(_gen(31), cache, dtype, 5, T, 2, 4, d, bt, lens)
     # ... with the weight of the softmax at one end, which most slices are far from
     q = q * 3
     q = q.to(R.TORCH[dtype])
-    _say(f"cache attention {cache} {dtype} d={d} bt={bt} in slices")
+    _say(f"cache attention {cache} {dtype} d={d} bt={bt} T={T} in slices")
     B.tir_set_workspace(None)
     alone = _check_attention(pool, table, q, lens, None, d ** -0.5, dtype, "f32", "one workgroup")
     ws = torch.full((B.tir_workspace_bytes(),), 255, dtype=torch.uint8, device="cuda")
