@@ -117,63 +117,67 @@ template <int DT> __device__ __forceinline__ f32x8 finite8(const uint4& w) {
 
 constexpr int kAppendThreads = 256;
 
-template <int DT, int CT, int DH, bool KEYS> __device__ __forceinline__ void append_side(const AppendParams& p) {
+template <int DT, int CT, int DH, int BT, bool KEYS> __device__ __forceinline__ void append_side(const AppendParams& p) {
     const int bj = (int)fastdiv(blockIdx.x, p.div_h_magic, p.div_h_shift);
     const int h = (int)blockIdx.x - bj * p.c.heads;
     const int b = (int)fastdiv((unsigned)bj, p.div_t_magic, p.div_t_shift);
     const int j = bj - b * p.touched;
-    const int bt = 1 << p.c.shift;
-    float* scale = KEYS ? p.c.ks : p.c.vs;
-    const long long rs = 2 * (KEYS ? p.k_rs : p.v_rs);
-    // positions lo .. hi - 1 of the sequence are this block's new tokens
+    // positions first + lo .. first + hi - 1 of the sequence are this block's new tokens
     int start = p.start[b], cnt = p.count ? p.count[b] : p.T;
     start = start < 0 ? 0 : start;
     cnt = cnt < 0 ? 0 : (cnt > p.T ? p.T : cnt);
-    const long long col = (long long)(start >> p.c.shift) + j;
+    const long long col = (long long)(start / BT) + j;
     if (col >= p.c.cols) return;
-    const long long first = col << p.c.shift;
+    const long long first = col * BT;
     const int lo = first > start ? 0 : (int)(start - first);                       // in the block
     const long long left = (long long)start + cnt - first;
-    const int hi = left >= bt ? bt : (int)(left < 0 ? 0 : left);
+    const int hi = left >= BT ? BT : (int)(left < 0 ? 0 : left);
     if (hi <= lo) return;
     const int id = p.c.table[(long long)b * p.c.cols + col];
-    if (id < 0 || id >= p.c.blocks) return;
-    const long long bh = (long long)id * p.c.heads + h;
-    scale += bh;
-    char* const tile = (KEYS ? p.c.k : p.c.v) + ((bh * DH) << p.c.shift);
+    const long long rs = 2 * (KEYS ? p.k_rs : p.v_rs);
     // (token 0 of the block, which need not be a new one)
     const char* const src = (const char*)(KEYS ? p.K : p.V) + 2 * (b * (KEYS ? p.k_bs : p.v_bs) + h * (KEYS ? p.k_hs : p.v_hs)) + (first - start) * rs;
 
     // A thread's units.  Keys: 16 channels of one token, so that rows are read and written whole.  Values: 8 channels of 4 tokens, which are
     // one word of each of 8 of the tile's rows.  Either is two to four 16-byte loads, and 128 tokens of 128 channels are four or two units per thread.
-    constexpr int UK = 128 * DH / 16 / kAppendThreads, UV = 128 / 4 * DH / 8 / kAppendThreads;
-    constexpr int KC = DH / 16;
-    uint4 w[2 * UK];
-    static_assert(2 * UK == 4 * UV, "");
-    if constexpr (KEYS) {
+    constexpr int UNITS = KEYS ? BT * DH / 16 : BT / 4 * DH / 8, U = (UNITS + kAppendThreads - 1) / kAppendThreads, L = KEYS ? 2 : 4;
+    constexpr int KC = DH / 16, VG = BT / 4;
+    uint4 w[U * L];
 #pragma unroll
-        for (int u = 0; u < UK; ++u) {
-            const int q = (int)threadIdx.x + u * kAppendThreads, tok = q / KC, c = q % KC;
-            const bool in = tok >= lo && tok < hi;
+    for (int u = 0; u < U; ++u) {
+        const int q = (int)threadIdx.x + u * kAppendThreads;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) w[2 * u + e] = in ? *(const uint4*)(src + tok * rs + c * 32 + e * 16) : make_uint4(0, 0, 0, 0);
+        for (int e = 0; e < L; ++e) {
+            const int tok = KEYS ? q / KC : q % VG * 4 + e;
+            const int at = KEYS ? q % KC * 32 + e * 16 : q / VG * 16;
+            w[u * L + e] = q < UNITS && tok >= lo && tok < hi ? *(const uint4*)(src + tok * rs + at) : make_uint4(0, 0, 0, 0);
         }
-    } else {
+    }
+    // (requested before the block's id is looked at: for a single token each trip to memory that waits for another is a fifth of the call)
+    TIR_FENCE();
+    if (id < 0 || id >= p.c.blocks) return;
+    const long long bh = (long long)id * p.c.heads + h;
+    float* const scale = (KEYS ? p.c.ks : p.c.vs) + bh;
+    char* const tile = (KEYS ? p.c.k : p.c.v) + bh * (DH * BT);
+    float was = 0.f;
+    if (lo > 0) was = *scale;
+    // words of values that are only partly new
+    u32x4 part[KEYS ? 1 : 2 * U];
+    if constexpr (!KEYS) {
 #pragma unroll
-        for (int u = 0; u < UV; ++u) {
-            const int q = (int)threadIdx.x + u * kAppendThreads, grp = q & (bt / 4 - 1), c = q >> (p.c.shift - 2);
+        for (int u = 0; u < U; ++u) {
+            const int q = (int)threadIdx.x + u * kAppendThreads, t0 = q % VG * 4;
+            part[2 * u] = part[2 * u + 1] = u32x4{0, 0, 0, 0};
+            if (q < UNITS && t0 < hi && t0 + 4 > lo && (t0 < lo || t0 + 4 > hi)) {
+                const char* const at = tile + (q / VG * 8) * BT + t0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int tok = grp * 4 + e;
-                w[4 * u + e] = tok >= lo && tok < hi && c < DH / 8 ? *(const uint4*)(src + tok * rs + c * 16) : make_uint4(0, 0, 0, 0);
+                for (int i = 0; i < 8; ++i) part[2 * u + i / 4][i % 4] = *(const unsigned*)(at + i * BT);
             }
         }
     }
-    float was = 0.f;
-    if (lo > 0) was = *scale;
     float top = 0.f;
 #pragma unroll
-    for (int i = 0; i < 2 * UK; ++i) {
+    for (int i = 0; i < U * L; ++i) {
         const f32x8 f = finite8<DT>(w[i]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) top = __builtin_fmaxf(top, __builtin_fabsf(f[e]));
@@ -182,7 +186,9 @@ template <int DT, int CT, int DH, bool KEYS> __device__ __forceinline__ void app
     for (int s = 1; s < 64; s <<= 1) top = __builtin_fmaxf(top, __shfl_xor(top, s));
     __shared__ float tops[kAppendThreads / 64];
     if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
-    __syncthreads();                                     // (everybody has read the old scale, too)
+    const bool held = lo > 0;
+    asm volatile("" : "+v"(was));                        // (the old scale is here before anybody writes the new one)
+    __syncthreads();
 #pragma unroll
     for (int i = 0; i < kAppendThreads / 64; ++i) top = __builtin_fmaxf(top, tops[i]);
     float now = top * cache_step<CT>();
@@ -190,15 +196,16 @@ template <int DT, int CT, int DH, bool KEYS> __device__ __forceinline__ void app
     now = __builtin_fmaxf(now, was);
     const float inv = 1.0f / now;
     const float ratio = was * inv;
-    const bool grew = now > was && lo > 0;
-    if (threadIdx.x == 0 && now != was) *scale = now;
+    const bool grew = now > was && held;
+    if (threadIdx.x == 0 && !(now == was && held)) *scale = now;
 
-    if constexpr (KEYS) {
 #pragma unroll
-        for (int u = 0; u < UK; ++u) {
-            const int q = (int)threadIdx.x + u * kAppendThreads, tok = q / KC, c = q % KC;
+    for (int u = 0; u < U; ++u) {
+        const int q = (int)threadIdx.x + u * kAppendThreads;
+        if constexpr (KEYS) {
+            const int tok = q / KC, c = q % KC;
             uint4* const dst = (uint4*)(tile + tok * DH + c * 16);
-            if (tok >= lo && tok < hi) {
+            if (q < UNITS && tok >= lo && tok < hi) {
                 const f32x8 f = finite8<DT>(w[2 * u]), e = finite8<DT>(w[2 * u + 1]);
                 *dst = make_uint4(to_eight<CT>(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv), to_eight<CT>(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv),
                                   to_eight<CT>(e[0] * inv, e[1] * inv, e[2] * inv, e[3] * inv), to_eight<CT>(e[4] * inv, e[5] * inv, e[6] * inv, e[7] * inv));
@@ -206,42 +213,40 @@ template <int DT, int CT, int DH, bool KEYS> __device__ __forceinline__ void app
                 const uint4 t = *dst;
                 *dst = make_uint4(requantise<CT>(t.x, ratio), requantise<CT>(t.y, ratio), requantise<CT>(t.z, ratio), requantise<CT>(t.w, ratio));
             }
-        }
-    } else {
-#pragma unroll
-        for (int u = 0; u < UV; ++u) {
-            const int q = (int)threadIdx.x + u * kAppendThreads, grp = q & (bt / 4 - 1), c = q >> (p.c.shift - 2);
-            const int t0 = grp * 4;
-            if (c < DH / 8 && t0 < hi && (t0 + 4 > lo || grew)) {
-                // bytes of the word that are new, and that are held
-                unsigned fresh = 0, held = 0;
+        } else {
+            const int t0 = q % VG * 4;
+            char* const dst = tile + (q / VG * 8) * BT + t0;
+            if (q < UNITS && t0 < hi && t0 + 4 > lo) {
+                // bytes of the word that are new, and that are held and have to be rounded again
+                unsigned fresh = 0, again = 0;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     if (t0 + e >= lo && t0 + e < hi) fresh |= 255u << (8 * e);
-                    if (t0 + e < lo) held |= 255u << (8 * e);
+                    if (t0 + e < lo && grew) again |= 255u << (8 * e);
                 }
-                char* const dst = tile + ((c * 8) << p.c.shift) + t0;
                 const f32x8 f0 = finite8<DT>(w[4 * u]), f1 = finite8<DT>(w[4 * u + 1]), f2 = finite8<DT>(w[4 * u + 2]), f3 = finite8<DT>(w[4 * u + 3]);
-                const unsigned again = grew ? held : 0u;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    unsigned* const at = (unsigned*)(dst + (i << p.c.shift));
                     const unsigned o = to_eight<CT>(f0[i] * inv, f1[i] * inv, f2[i] * inv, f3[i] * inv);
-                    if (fresh == ~0u) {
-                        *at = o;
-                    } else {
-                        const unsigned was8 = *at, kept = (was8 & ~again) | (requantise<CT>(was8, ratio) & again);
-                        *at = (kept & ~fresh) | (o & fresh);
-                    }
+                    const unsigned old = part[2 * u + i / 4][i % 4];
+                    unsigned kept = old;
+                    if (again) kept = (old & ~again) | (requantise<CT>(old, ratio) & again);
+                    *(unsigned*)(dst + i * BT) = (kept & ~fresh) | (o & fresh);
+                }
+            } else if (grew && q < UNITS && t0 + 4 <= lo) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    unsigned* const at = (unsigned*)(dst + i * BT);
+                    *at = requantise<CT>(*at, ratio);
                 }
             }
         }
     }
 }
 
-template <int DT, int CT, int DH> __global__ void __launch_bounds__(kAppendThreads) cache_append_kernel(const AppendParams p) {
-    if (blockIdx.y == 0) append_side<DT, CT, DH, true>(p);
-    else append_side<DT, CT, DH, false>(p);
+template <int DT, int CT, int DH, int BT> __global__ void __launch_bounds__(kAppendThreads) cache_append_kernel(const AppendParams p) {
+    if (blockIdx.y == 0) append_side<DT, CT, DH, BT, true>(p);
+    else append_side<DT, CT, DH, BT, false>(p);
 }
 
 // ---------------------------------------------------------------------------------------------

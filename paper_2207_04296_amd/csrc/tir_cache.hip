@@ -9,7 +9,11 @@
 namespace tir {
 
 template <int DT, int CT, int DH> static hipError_t launch_append_as(const AppendParams& p, int64_t batch, hipStream_t stream) {
-    return launch_kernel(&cache_append_kernel<DT, CT, DH>, dim3((unsigned)(batch * p.touched * p.c.heads), 2), dim3(kAppendThreads), stream, p);
+    const dim3 grid((unsigned)(batch * p.touched * p.c.heads), 2), block(kAppendThreads);
+    if (p.c.shift == 4) return launch_kernel(&cache_append_kernel<DT, CT, DH, 16>, grid, block, stream, p);
+    if (p.c.shift == 5) return launch_kernel(&cache_append_kernel<DT, CT, DH, 32>, grid, block, stream, p);
+    if (p.c.shift == 6) return launch_kernel(&cache_append_kernel<DT, CT, DH, 64>, grid, block, stream, p);
+    return launch_kernel(&cache_append_kernel<DT, CT, DH, 128>, grid, block, stream, p);
 }
 hipError_t launch_append(const AppendParams& p, int dt, int ct, int d, int64_t batch, hipStream_t stream) {
 #define TIR_APPEND(DT, CT, DH) if (dt == DT && ct == CT && d == DH) return launch_append_as<DT, CT, DH>(p, batch, stream);
@@ -60,10 +64,13 @@ static void choose_cache_kernel(CacheAttnParams* p, int64_t d, const StreamWorks
         tiles = tall;
         slices = tall_slices;
     } else if (ws.partial && tiles <= ws.counters && tiles < 512) {
-        // four waves with two chunks of 32 keys each, or one of 64
-        const int64_t small = p->rows_of_tile == 32 ? part : d == 64 ? token_partial_bytes<64>() : token_partial_bytes<128>();
-        slices = (512 + tiles - 1) / tiles;
-        if (slices > (keys + 255) / 256) slices = (keys + 255) / 256;
+        // Tiles of 16 rows: as many workgroups as CUs, with two chunks of 64 keys per wave.  256 and 512 workgroups in all, us: one token over 30 000 20.8 / 25.3, over 200 003 87 / 96, 32 x 2000 20.3 / 24.0;
+        // one chunk per wave 8 x 2000 15.9, two 14.2.  Tiles of 32: twice the workgroups, two chunks of 32 (8 x 20 tokens over 3000 27.1 us, 33.9 with one workgroup per CU and four).
+        const bool token = p->rows_of_tile == 16;
+        const int64_t small = !token ? part : d == 64 ? token_partial_bytes<64>() : token_partial_bytes<128>();
+        const int64_t room = token ? 256 : 512, least = token ? 512 : 256;
+        slices = (room + tiles - 1) / tiles;
+        if (slices > (keys + least - 1) / least) slices = (keys + least - 1) / least;
         if (slices > 64) slices = 64;
         if (slices > ws.bytes / (tiles * small)) slices = ws.bytes / (tiles * small);
         if (slices < 1) slices = 1;

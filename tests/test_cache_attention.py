@@ -330,8 +330,8 @@ def test_the_tall_calls_take_the_tall_tiles():
     for batch, heads, group, d, bt, T, lens, count, kernel in TALL:
         assert B.tir_debug_cache_kernel(batch, T, heads * group, heads, d, bt, -(-max(lens) // bt) + 1) == kernel
     assert B.tir_debug_cache_kernel(64, 1, 32, 8, 128, 64, 128) == "rows16/z1"
-    assert B.tir_debug_cache_kernel(1, 1, 32, 8, 128, 128, 1563) == "rows16/z64"
-    assert B.tir_debug_cache_kernel(2, 5, 16, 4, 64, 16, 100) == "rows32/z7" and B.tir_debug_cache_kernel(2, 4, 16, 4, 64, 16, 100) == "rows16/z7"
+    assert B.tir_debug_cache_kernel(1, 1, 32, 8, 128, 128, 1563) == "rows16/z32"
+    assert B.tir_debug_cache_kernel(2, 5, 16, 4, 64, 16, 100) == "rows32/z7" and B.tir_debug_cache_kernel(2, 4, 16, 4, 64, 16, 100) == "rows16/z4"
 
 
 @pytest.mark.gpu
