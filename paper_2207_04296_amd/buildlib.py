@@ -19,7 +19,7 @@ OBJ = PKG / "_build"
 LIB = PKG / "libtir.so"
 NATIVE = PKG / "_native.so"
 N_UNITS = 6
-UNITS = ["tir_cache", "tir_cross", "tir_cross_grad"]      # the decoder's attentions: one translation unit each
+UNITS = ["tir_cache", "tir_cross", "tir_cross_token", "tir_cross_grad"]      # the decoder's attentions: one translation unit each
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-but-set-variable",

@@ -36,6 +36,7 @@ struct CrossParams : AttnParams {      // M: positions * G, N: largest number of
     const int* lens;         // keys of each sequence; null: N each
     float* lse;              // [sequences][query heads][positions], or null
     int heads, G, positions;      // key heads, query heads per key head, rows of a query head
+    int out32;               // fp32 output (the form for a few rows; the others' output type is compiled)
     int slices;              // workgroups that share a tile's keys
     void* ws;                // slices > 1: partial results [tile][slice][kernel's MERGE * QW]
     unsigned* ws_count;      // ... and arrival counters [tile], zero between launches

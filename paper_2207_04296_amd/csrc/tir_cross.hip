@@ -3,6 +3,7 @@
 #include <stdint.h>
 
 #include "tir_attention.h"
+#include "tir_cross_token.h"
 #include "tir_host.h"
 #include "tir_launch.h"
 
@@ -87,21 +88,30 @@ tir_status tir_cross_attention(const void* Q, const void* K, const void* V, void
     const FastDiv dh = make_fastdiv((unsigned)p.heads), dg = make_fastdiv((unsigned)p.G);
     p.div_h_magic = dh.magic; p.div_h_shift = dh.shift;
     p.div_g_magic = dg.magic; p.div_g_shift = dg.shift;
-    // Few tiles of 64 rows: their keys are shared among workgroups, one of which fills a CU, as long as each of its four key groups keeps two chunks.
+    p.out32 = out == TIR_F32;
     p.slices = 1;
-    const int64_t tiles = (int64_t)p.batch * ((p.M + 63) / 64), chunk = d == 64 ? 64 : 32;
-    if (tiles <= 128 && N >= 16 * chunk) {
-        const StreamWorkspace ws = stream_workspace((hipStream_t)stream);
-        int64_t slices = 256 / tiles;
-        if (slices > N / (8 * chunk)) slices = N / (8 * chunk);
+    const StreamWorkspace ws = stream_workspace((hipStream_t)stream);
+    auto share = [&](int64_t tiles, int64_t slices, int64_t most, int64_t part) {
+        if (slices > most) slices = most;
         if (slices > 64) slices = 64;
-        if (ws.partial && tiles <= ws.counters && slices > 1 && slices * tiles * 2 * (d / 32 * 4096 + 512) <= ws.bytes) {
+        if (ws.partial && tiles <= ws.counters && slices > 1 && slices * tiles * part <= ws.bytes) {
             p.slices = (int)slices;
             p.ws = ws.partial;
             p.ws_count = ws.count;
         }
+    };
+    hipError_t e;
+    if (p.M <= kTokenRows && N > 0) {
+        const int64_t chunk = d == 64 ? 32 : 16;         // two per wave
+        share(p.batch, 256 / p.batch, N / (8 * chunk), d == 64 ? cross_token_partial<64>(p.M) : cross_token_partial<128>(p.M));
+        e = launch_cross_token(p, (int)in, (int)d, (hipStream_t)stream);
+        if (e != hipSuccess) return host_error(TIR_ERR_LAUNCH, "%s: launch failed: %s", who, hipGetErrorString(e));
+        return TIR_OK;
     }
-    const hipError_t e = fn(p, (hipStream_t)stream);
+    // Few tiles of 64 rows: their keys are shared among workgroups, one of which fills a CU, as long as each of its four key groups keeps two chunks.
+    const int64_t tiles = (int64_t)p.batch * ((p.M + 63) / 64), chunk = d == 64 ? 64 : 32;
+    if (tiles <= 128) share(tiles, 256 / tiles, N / (8 * chunk), 2 * (d / 32 * 4096 + 512));
+    e = fn(p, (hipStream_t)stream);
     if (e != hipSuccess) return host_error(TIR_ERR_LAUNCH, "%s: launch failed: %s", who, hipGetErrorString(e));
     return TIR_OK;
 }

@@ -122,6 +122,7 @@ def workspace():
 SHAPES = [
     (2, 1, 1, 1, 1, None), (1, 1, 700, 2, 1, None), (3, 1, 333, 2, 4, [333, 0, 100]), (2, 33, 65, 1, 3, [65, 1]), (2, 130, 77, 2, 1, None), (4, 7, 200, 3, 2, [200, 64, 63, 65]),
     (1, 300, 129, 1, 1, [128]), (2, 64, 500, 1, 2, [-3, 10000]), (40, 50, 40, 4, 1, None), (1, 257, 1030, 1, 1, None),
+    (2, 1, 90, 3, 2, None), (3, 3, 50, 2, 1, [50, 0, 17]), (2, 2, 31, 1, 2, [31, 1]), (2, 5, 40, 2, 1, None),
 ]
 
 
@@ -232,13 +233,14 @@ def test_broadcast_inputs_strides_and_rows_behind(workspace):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("d", [64, 128])
-def test_keys_shared_among_workgroups(d):
-    """Single tokens over many keys, with and without a workspace: the slices did run, and the same call gives the same bits."""
+@pytest.mark.parametrize("m,group", [(1, 4), (1, 1), (3, 4)])
+def test_keys_shared_among_workgroups(d, m, group):
+    """Few rows over many keys, with and without a workspace: the slices did run, and the same call gives the same bits."""
     import torch
     lens = [7000, 0, 1, 5000]
-    q, kv = _inputs(_gen(13), "bf16", 4, 1, 7000, 2, 4, d, lens)
+    q, kv = _inputs(_gen(13), "bf16", 4, m, 7000, 2, group, d, lens)
     q = (q * 2).to(q.dtype)
-    _say(f"cross attention in slices, d={d}")
+    _say(f"cross attention in slices, m={m} group={group} d={d}")
     B.tir_set_workspace(None)
     alone, _ = _check(q, kv, lens, d ** -0.5, "bf16", "f32", "one workgroup")
     ws = torch.full((B.tir_workspace_bytes(),), 255, dtype=torch.uint8, device="cuda")
