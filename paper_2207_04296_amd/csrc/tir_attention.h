@@ -35,6 +35,7 @@ struct CrossParams : AttnParams {      // M: positions * G, N: largest number of
     long long q_bs, q_rs, q_hs, k_bs, k_rs, k_hs, v_bs, v_rs, v_hs, o_bs, o_rs, o_hs;      // in elements
     const int* lens;         // keys of each sequence; null: N each
     float* lse;              // [sequences][query heads][positions], or null
+    int o_near;              // 256 positions and all heads of a group lie within 2^31 bytes of O
     int heads, G, positions;      // key heads, query heads per key head, rows of a query head
     int out32;               // fp32 output (the form for a few rows; the others' output type is compiled)
     int slices;              // workgroups that share a tile's keys
@@ -657,11 +658,24 @@ __global__ void __launch_bounds__(QW * KG * 64, 2) attention_kernel(const P p) {
     __syncthreads();
     if constexpr (CROSS) {
         constexpr int ORC = ORB / 16;
+        typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+        // Written through like every output (4 x 4096 x 77 x 8 heads of 64: 13.1 us with the default policy, whose dirty lines leave the caches at the end of the kernel), from the tile's first position on,
+        // which is as far as 31 bits have to reach; strides beyond that are stored plainly.
+        const int first_m = (int)fastdiv((unsigned)m0, p.div_g_magic, p.div_g_shift);
+        out_t* const Ob = (out_t*)p.O + seq * p.o_bs + (long long)head * p.G * p.o_hs + first_m * p.o_rs;
+        const __amdgpu_buffer_rsrc_t ro = __builtin_amdgcn_make_buffer_rsrc((void*)Ob, 0, 0x7fffffff, 0x00020000);
 #pragma unroll
         for (int i = 0; i < TQ * ORC / (GT * KG); ++i) {
             const int q = (int)threadIdx.x + i * GT * KG;
             const int row = q / ORC, pc = q % ORC;
-            if (row < rows_q) *(uint4*)((out_t*)p.O + row_at(row, p.o_bs, p.o_rs, p.o_hs) + pc * (16 / OS)) = *(const uint4*)(s_o + row * ORB + ((pc * 16) ^ ((row & 7) << 4)));
+            const u32x4 v = *(const u32x4*)(s_o + row * ORB + ((pc * 16) ^ ((row & 7) << 4)));
+            if (p.o_near) {
+                const int m = (int)fastdiv((unsigned)(m0 + row), p.div_g_magic, p.div_g_shift);
+                const int at = ((m - first_m) * (int)p.o_rs + (m0 + row - m * p.G) * (int)p.o_hs + pc * (16 / OS)) * OS;
+                __builtin_amdgcn_raw_buffer_store_b128(v, ro, row < rows_q ? at : (int)kOutOfRange, 0, TIR_STORE_AUX);
+            } else if (row < rows_q) {
+                *(u32x4*)((out_t*)p.O + row_at(row, p.o_bs, p.o_rs, p.o_hs) + pc * (16 / OS)) = v;
+            }
         }
     } else {
         char* Ob = (char*)p.O + (b * p.M + m0) * (long long)ORB;

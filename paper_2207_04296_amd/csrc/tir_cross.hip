@@ -89,6 +89,7 @@ tir_status tir_cross_attention(const void* Q, const void* K, const void* V, void
     p.div_h_magic = dh.magic; p.div_h_shift = dh.shift;
     p.div_g_magic = dg.magic; p.div_g_shift = dg.shift;
     p.out32 = out == TIR_F32;
+    p.o_near = o_rs < (1 << 20) && o_hs < (1 << 28) / p.G;      // (257 * o_rs + G * o_hs + d) * 4 < 2^31
     p.slices = 1;
     const StreamWorkspace ws = stream_workspace((hipStream_t)stream);
     auto share = [&](int64_t tiles, int64_t slices, int64_t most, int64_t part) {

@@ -25,6 +25,7 @@ struct GradParams {
     float* delta;            // the same: D, written by the pass over rows
     const int* lens;         // null: N each
     long long q_bs, q_rs, q_hs, k_bs, k_rs, k_hs, v_bs, v_rs, v_hs, o_bs, o_rs, o_hs, g_bs, g_rs, g_hs;      // (g: dO)
+    int q_near;              // 128 positions and all heads of a group lie within 2^31 bytes of dQ
     int M, N, heads, G;      // key heads, query heads per key head
     int batch, tiles;        // tiles of rows resp. keys of a (sequence, key head)
     int slices;              // workgroups that share a tile's walk: partial sums in ws, added by grad_sum_kernel
@@ -151,6 +152,22 @@ template <int DT, int DB> __device__ __forceinline__ void round_ds(f32x16& ds, f
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) w[i] = grad_pack<DT>(ds[2 * i], ds[2 * i + 1]);
+    }
+}
+// Four values of a row into a tile of rows in LDS, and that tile to memory in 16-byte pieces: a row's values lie in two lanes, 8 bytes at a time.  Written through (see the forward kernels);
+// `near`: the tile's rows lie within 2^31 bytes.  place(r): elements from base to row r.  Threads of the workgroup (T = its size) or of a wave (64) take part.
+template <int DH> __device__ __forceinline__ void grad_stage(char* tile, int row, int ch, uint2 v) { *(uint2*)(tile + row * (DH * 2) + ((ch * 2) ^ ((row & 7) << 4))) = v; }
+template <int DH, int T, class PLACE> __device__ __forceinline__ void grad_store(const char* tile, unsigned short* base, int rows, bool near, PLACE place) {
+    typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+    constexpr int RC = DH / 8, ROWS = T == 64 ? 32 : kGradTile;      // 16-byte pieces of a row
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, 0x7fffffff, 0x00020000);
+#pragma unroll
+    for (int i = 0; i < ROWS * RC / T; ++i) {
+        const int q = (int)(threadIdx.x & (T - 1)) + i * T, row = q / RC, pc = q % RC;
+        const u32x4 v = *(const u32x4*)(tile + row * (DH * 2) + ((pc * 16) ^ ((row & 7) << 4)));
+        const long long at = place(row) + pc * 8;
+        if (near) __builtin_amdgcn_raw_buffer_store_b128(v, r, row < rows ? (int)at * 2 : (int)kOutOfRange, 0, TIR_STORE_AUX);
+        else if (row < rows) *(u32x4*)(base + at) = v;
     }
 }
 constexpr float kFirstFactor = 0x1p100f;      // before any dS has been seen
@@ -290,13 +307,20 @@ __global__ void __launch_bounds__(kGradThreads, 2) grad_rows_kernel(const GradPa
             for (int q4 = 0; q4 < 4; ++q4) o[(db * 4 + q4) * 64] = f32x4{acc[db][4 * q4] * f, acc[db][4 * q4 + 1] * f, acc[db][4 * q4 + 2] * f, acc[db][4 * q4 + 3] * f};
         return;
     }
-    if (!live) return;
-    unsigned short* const out = (unsigned short*)p.dQ + b * p.q_bs + m * p.q_rs + hq * p.q_hs;
+    __syncthreads();                           // the rings are free
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
         for (int q4 = 0; q4 < 4; ++q4)
-            *(uint2*)(out + db * 32 + q4 * 8 + 4 * g) = make_uint2(grad_pack<DT>(acc[db][4 * q4] * f, acc[db][4 * q4 + 1] * f), grad_pack<DT>(acc[db][4 * q4 + 2] * f, acc[db][4 * q4 + 3] * f));
+            grad_stage<DH>(smem, wave * 32 + l31, db * 32 + q4 * 8 + 4 * g,
+                           make_uint2(grad_pack<DT>(acc[db][4 * q4] * f, acc[db][4 * q4 + 1] * f), grad_pack<DT>(acc[db][4 * q4 + 2] * f, acc[db][4 * q4 + 3] * f)));
+    __syncthreads();
+    const int first_m = (int)fastdiv((unsigned)row0, p.div_g_magic, p.div_g_shift);
+    unsigned short* const base = (unsigned short*)p.dQ + b * p.q_bs + (long long)h * p.G * p.q_hs + first_m * p.q_rs;
+    grad_store<DH, kGradThreads>(smem, base, rows, p.q_near != 0, [&](int r) __attribute__((always_inline)) -> long long {
+        const int mr = (int)fastdiv((unsigned)(row0 + r), p.div_g_magic, p.div_g_shift);
+        return (mr - first_m) * p.q_rs + (row0 + r - mr * p.G) * p.q_hs;
+    });
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -483,6 +507,8 @@ __global__ void __launch_bounds__(kGradThreads * RG, 2) grad_keys_kernel(const G
                 dv[db][r] *= fv;
             }
     }
+    char* const stage = smem + wave * (RG == 1 ? 32 * DH * 2 : MERGE);      // this wave's place for the 32 rows that it stores: where it read the other group's sums, or the first rings
+    static_assert(RG > 1 || kGradWaves * 32 * DH * 2 <= LDS, "");
     if (p.slices > 1) {
         f32x4* const o = (f32x4*)p.ws + ((long long)blockIdx.x * p.slices + blockIdx.y) * (2 * kGradTile * DH / 4) + wave * (32 * DH / 4) + lane;
 #pragma unroll
@@ -494,19 +520,23 @@ __global__ void __launch_bounds__(kGradThreads * RG, 2) grad_keys_kernel(const G
             }
         return;
     }
-    if (key >= p.N) return;
-    unsigned short* const ok = (unsigned short*)p.dK + b * p.k_bs + key * p.k_rs + h * p.k_hs;
-    unsigned short* const ov = (unsigned short*)p.dV + b * p.v_bs + key * p.v_rs + h * p.v_hs;
+    // keys behind the sequence's have zeros
+    auto store = [&](const f32x16 (&x)[DB], void* to, long long bs, long long rs, long long hs) __attribute__((always_inline)) {
+        if constexpr (RG == 1) __syncthreads();          // the rings are free (the merged groups' values that were read last are each wave's own)
+        else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
+        for (int db = 0; db < DB; ++db)
 #pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4) {
-            const int at = db * 32 + q4 * 8 + 4 * g;
-            const uint2 x = make_uint2(grad_pack<DT>(dk[db][4 * q4], dk[db][4 * q4 + 1]), grad_pack<DT>(dk[db][4 * q4 + 2], dk[db][4 * q4 + 3]));
-            const uint2 y = make_uint2(grad_pack<DT>(dv[db][4 * q4], dv[db][4 * q4 + 1]), grad_pack<DT>(dv[db][4 * q4 + 2], dv[db][4 * q4 + 3]));
-            *(uint2*)(ok + at) = live ? x : make_uint2(0, 0);
-            *(uint2*)(ov + at) = live ? y : make_uint2(0, 0);
-        }
+            for (int q4 = 0; q4 < 4; ++q4) {
+                const uint2 v = make_uint2(grad_pack<DT>(x[db][4 * q4], x[db][4 * q4 + 1]), grad_pack<DT>(x[db][4 * q4 + 2], x[db][4 * q4 + 3]));
+                grad_stage<DH>(stage, l31, db * 32 + q4 * 8 + 4 * g, live ? v : make_uint2(0, 0));
+            }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        const int first = key0 + wave * 32;
+        grad_store<DH, 64>(stage, (unsigned short*)to + b * bs + first * rs + h * hs, p.N - first, true, [&](int r) __attribute__((always_inline)) -> long long { return r * rs; });
+    };
+    store(dk, p.dK, p.k_bs, p.k_rs, p.k_hs);
+    store(dv, p.dV, p.v_bs, p.v_rs, p.v_hs);
 }
 
 // ---------------------------------------------------------------------------------------------

@@ -83,6 +83,7 @@ tir_status tir_cross_attention_backward(const void* Q, const void* K, const void
     p.G = (int)(Hq / Hkv);
     p.batch = (int)batch;
     p.scale = scale;
+    p.q_near = q_rs < (1 << 20) && q_hs < (1 << 28) / p.G;      // (129 * q_rs + G * q_hs + d) * 2 < 2^31
     p.scale_log2e = scale * 1.44269504088896340736f;
     const FastDiv dh = make_fastdiv((unsigned)p.heads), dg = make_fastdiv((unsigned)p.G);
     p.div_h_magic = dh.magic; p.div_h_shift = dh.shift;

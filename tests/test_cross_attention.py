@@ -232,6 +232,24 @@ def test_broadcast_inputs_strides_and_rows_behind(workspace):
 
 
 @pytest.mark.gpu
+def test_outputs_with_far_strides():
+    """Rows 2^21 elements apart, further than a tile is addressed with 31 bits, and heads 2^20 apart; nothing between them changes."""
+    import torch
+    q, kv = _inputs(_gen(23), "f16", 1, 40, 90, 2, 1, 64, None)
+    qd, kvd = _to_device(q), _to_device(kv)
+    k, v = kvd[:, :, 0], kvd[:, :, 1]
+    flat = torch.full((40 << 21,), MARK, dtype=torch.float16, device="cuda")
+    o = flat.as_strided((1, 40, 2, 64), (40 << 21, 1 << 21, 1 << 20, 1))
+    _say("cross attention, far rows")
+    B.tir_cross_attention(qd, k, v, o, None, None, 1, 40, 90, 2, 2, 64, *qd.stride()[:3], *k.stride()[:3], *v.stride()[:3], *o.stride()[:3], 0.125, "f16", "f16")
+    torch.cuda.synchronize()
+    ref = R.cross_attention(q, kv[:, :, 0], kv[:, :, 1], None, 0.125)
+    assert torch.all((o.cpu().double() - ref["o"]).abs() <= _tolerance(ref["T"], ref["o"], "f16", "f16"))
+    o.fill_(MARK)
+    assert bool((flat == MARK).all())
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("m,group", [(1, 4), (1, 1), (3, 4)])
 def test_keys_shared_among_workgroups(d, m, group):

@@ -230,6 +230,38 @@ def test_gradients_that_arrive_in_other_orders(workspace):
 
 
 @pytest.mark.gpu
+def test_gradients_with_far_strides():
+    """Queries (and so their gradients) 2^21 elements apart, keys 2^19: nothing between the rows changes."""
+    import torch
+    m, n = 40, 90
+    q, kv = _inputs(_gen(29), "f16", 1, m, n, 2, 1, 64, None)
+    do = torch.randn(q.shape, generator=_gen(31)).to(torch.float16)
+    ref = R.cross_attention(q, kv[:, :, 0], kv[:, :, 1], None, 0.125, do)
+    far = {}
+    for name, x, rs in (("q", q, 1 << 21), ("k", kv[:, :, 0], 1 << 19), ("v", kv[:, :, 1], 1 << 19), ("dq", None, 1 << 21), ("dk", None, 1 << 19), ("dv", None, 1 << 19)):
+        rows = m if name in ("q", "dq") else n
+        flat = torch.full((rows * rs,), MARK, dtype=torch.float16, device="cuda")
+        view = flat.as_strided((1, rows, 2, 64), (rows * rs, rs, rs // 2, 1))
+        if x is not None:
+            view.copy_(x)
+        far[name] = (flat, view)
+    qd, k, v, dq, dk, dv = (far[x][1] for x in ("q", "k", "v", "dq", "dk", "dv"))
+    dod = do.cuda()
+    o, lse, delta = torch.empty_like(dod), torch.empty((1, 2, m), device="cuda"), torch.empty((1, 2, m), device="cuda")
+    strides = (*qd.stride()[:3], *k.stride()[:3], *v.stride()[:3], *o.stride()[:3])
+    _say("gradients, far rows")
+    B.tir_cross_attention(qd, k, v, o, lse, None, 1, m, n, 2, 2, 64, *strides, 0.125, "f16", "f16")
+    B.tir_cross_attention_backward(qd, k, v, o, dod, lse, None, dq, dk, dv, delta, 1, m, n, 2, 2, 64, *strides, *dod.stride()[:3], 0.125, "f16")
+    torch.cuda.synchronize()
+    for x in ("dq", "dk", "dv"):
+        flat, view = far[x]
+        tol = 3 * U["f16"] * ref[x + "_sum"] + U["f16"] * ref[x].abs() + 1e-6
+        assert torch.all((view.cpu().double() - ref[x]).abs() <= tol), x
+        view.fill_(MARK)
+        assert bool((flat == MARK).all()), x
+
+
+@pytest.mark.gpu
 def test_no_queries_and_no_keys():
     import torch
     q, kv = _inputs(_gen(13), "f16", 2, 4, 6, 2, 1, 64, None)
