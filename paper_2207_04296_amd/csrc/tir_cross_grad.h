@@ -298,6 +298,7 @@ __global__ void __launch_bounds__(kGradThreads, 2) grad_rows_kernel(const GradPa
     }
     const float f = p.scale / by;
     if (p.slices > 1) {
+        if (wave * 32 >= rows) return;                   // (nobody reads these)
         // [tile][slice][wave][db][quarter][lane] of four values
         typedef float f32x4 __attribute__((ext_vector_type(4)));
         f32x4* const o = (f32x4*)p.ws + ((long long)blockIdx.x * p.slices + blockIdx.y) * (kGradTile * DH / 4) + wave * (32 * DH / 4) + lane;
@@ -510,6 +511,7 @@ __global__ void __launch_bounds__(kGradThreads * RG, 2) grad_keys_kernel(const G
     char* const stage = smem + wave * (RG == 1 ? 32 * DH * 2 : MERGE);      // this wave's place for the 32 rows that it stores: where it read the other group's sums, or the first rings
     static_assert(RG > 1 || kGradWaves * 32 * DH * 2 <= LDS, "");
     if (p.slices > 1) {
+        if (key0 + wave * 32 >= p.N) return;             // (nobody reads these)
         f32x4* const o = (f32x4*)p.ws + ((long long)blockIdx.x * p.slices + blockIdx.y) * (2 * kGradTile * DH / 4) + wave * (32 * DH / 4) + lane;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
@@ -546,18 +548,18 @@ template <int DT, int DH, bool KEYS> __global__ void __launch_bounds__(256) grad
     typedef float f32x4 __attribute__((ext_vector_type(4)));
     constexpr int PART = (KEYS ? 2 : 1) * kGradTile * DH / 4;
     const int tile = (int)blockIdx.y, at = (int)(blockIdx.x * 256 + threadIdx.x);      // < PART: a multiple of 256
-    const f32x4* const part = (const f32x4*)p.ws + (long long)tile * p.slices * PART + at;
-    f32x4 sum = part[0];
-#pragma unroll 4
-    for (int z = 1; z < p.slices; ++z) sum += part[(long long)z * PART];
     const int bh = (int)fastdiv((unsigned)tile, p.div_tiles_magic, p.div_tiles_shift);
     const int b = (int)fastdiv((unsigned)bh, p.div_h_magic, p.div_h_shift), h = bh - b * p.heads;
     const int in = at % (kGradTile * DH / 4), lane = in & 63, grp = in >> 6;       // grp = wave * (DH / 8) + db * 4 + quarter
     const int row = (tile - bh * p.tiles) * kGradTile + grp / (DH / 8) * 32 + (lane & 31);
     const int ch = grp % (DH / 8) * 8 + 4 * (lane >> 5);
+    if (row >= (KEYS ? p.N : p.M * p.G)) return;                                    // (what no pass writes)
+    const f32x4* const part = (const f32x4*)p.ws + (long long)tile * p.slices * PART + at;
+    f32x4 sum = part[0];
+#pragma unroll 4
+    for (int z = 1; z < p.slices; ++z) sum += part[(long long)z * PART];
     const uint2 v = make_uint2(grad_pack<DT>(sum[0], sum[1]), grad_pack<DT>(sum[2], sum[3]));
     if constexpr (KEYS) {
-        if (row >= p.N) return;
         int n = p.N;
         if (p.lens) {
             n = p.lens[b];
@@ -567,7 +569,6 @@ template <int DT, int DH, bool KEYS> __global__ void __launch_bounds__(256) grad
         unsigned short* const o = second ? (unsigned short*)p.dV + b * p.v_bs + row * p.v_rs + h * p.v_hs : (unsigned short*)p.dK + b * p.k_bs + row * p.k_rs + h * p.k_hs;
         *(uint2*)(o + ch) = row < n ? v : make_uint2(0, 0);
     } else {
-        if (row >= p.M * p.G) return;
         const int m = (int)fastdiv((unsigned)row, p.div_g_magic, p.div_g_shift), hq = h * p.G + row - m * p.G;
         *(uint2*)((unsigned short*)p.dQ + b * p.q_bs + m * p.q_rs + hq * p.q_hs + ch) = v;
     }
