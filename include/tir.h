@@ -192,9 +192,9 @@ tir_status tir_attention(const void* Q, const void* K, const void* V, void* O, i
  * 64 or 128 tokens of all `heads` key heads; a key or value is the stored 8-bit number (dtype: I8, or E4M3) times the scale
  * of its block and head.  Every array is dense:
  *     k [blocks][heads][block_tokens][d]      v [blocks][heads][d][block_tokens]  (a head's values transposed, tokens innermost)
- *     k_scale, v_scale [blocks][heads] fp32   table [batch][columns] int32
+ *     k_scale, v_scale [blocks][heads] fp32   table [sequences][columns] int32
  * Position j of sequence b is token j % block_tokens of block table[b][j / block_tokens].  d is 64 or 128; k and v are 16-byte aligned.  An entry of
- * the table outside [0, blocks) is a block that is not there.  columns * block_tokens < 2^31.
+ * the table outside [0, blocks) is a block that is not there.  columns * block_tokens is at most 2^31 - 2^16.
  * The caller owns all of it; the contents of a block that nothing was appended to are never used, nor are those of positions that hold no token.
  */
 typedef struct tir_kv_cache {
@@ -203,8 +203,9 @@ typedef struct tir_kv_cache {
     float* k_scale;
     float* v_scale;
     const int32_t* table;
-    int64_t blocks, heads, block_tokens, d, columns;
-    int32_t dtype; /* TIR_I8 or TIR_E4M3 */
+    int64_t blocks, heads, block_tokens, d;
+    int64_t sequences, columns; /* of the table: a call's batch is at most `sequences` */
+    int32_t dtype;              /* TIR_I8 or TIR_E4M3 */
 } tir_kv_cache;
 
 /*
@@ -250,7 +251,7 @@ tir_status tir_cache_attention(const void* Q, const tir_kv_cache* cache, void* O
  * hold.  A sequence without keys gives zeros.  lse: fp32 [batch][Hq][M], dense, log(sum_j exp(scale * Q.K)), -infinity without keys, which the backward pass
  * needs; NULL where it is not wanted.  in = F16 or BF16; out = the same type or F32.  Arithmetic and accuracy as tir_attention; lse to 1e-5 + 2^-22 * max|scale * Q.K|.
  * With a workspace registered for `stream` few queries over many keys are shared among workgroups, whose results are added in a fixed order.
- * Pointers 16-byte aligned, all strides multiples of 8 elements, row strides at most 2^23; those of O must keep its rows apart, those of the inputs may be 0.  batch, M or Hq = 0 is a no-op.
+ * Pointers 16-byte aligned, all strides multiples of 8 elements, row strides at most 2^23, N at most 2^31 - 2^16; the strides of O must keep its rows apart, those of the inputs may be 0.  batch, M or Hq = 0 is a no-op.
  */
 tir_status tir_cross_attention(const void* Q, const void* K, const void* V, void* O, float* lse, const int32_t* lens,
                                int64_t batch, int64_t M, int64_t N, int64_t Hq, int64_t Hkv, int64_t d, int64_t q_bs,
@@ -289,7 +290,9 @@ const char* tir_last_error(void);
  * the partial sums in `ws` (device memory, 256-byte aligned, at least tir_workspace_bytes() bytes, owned by the
  * caller).  The call enqueues one small kernel on `stream` that zeroes the counters (a kernel, not a memset, so
  * the call may be captured) and returns; every launch leaves them zero again.  The buffer must stay allocated
- * until the work enqueued on `stream` has finished and a later tir_set_workspace has replaced or removed it;
+ * until the work enqueued on `stream` has finished and a later tir_set_workspace has replaced or removed it (a graph
+ * captured from `stream` keeps using it: two graphs that may run at the same time are captured from streams with
+ * buffers of their own);
  * ws = NULL removes the registration (later launches on `stream` run unsplit).  Two streams that may run at the
  * same time need two buffers: launches that share one race.  Tuning calls use the workspace of the stream they
  * are given and try split reductions only if it has one.

@@ -45,13 +45,13 @@ def make_epilogue(bias=None, relu=False, scale=0.0, streaming=False):
 class KvCache(ctypes.Structure):
     """struct tir_kv_cache; make_kv_cache() fills one from tensors, which it keeps alive."""
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("table", ctypes.c_void_p),
-                ("blocks", ctypes.c_int64), ("heads", ctypes.c_int64), ("block_tokens", ctypes.c_int64), ("d", ctypes.c_int64), ("columns", ctypes.c_int64),
+                ("blocks", ctypes.c_int64), ("heads", ctypes.c_int64), ("block_tokens", ctypes.c_int64), ("d", ctypes.c_int64), ("sequences", ctypes.c_int64), ("columns", ctypes.c_int64),
                 ("dtype", ctypes.c_int32)]
 
 
 def make_kv_cache(k, v, k_scale, v_scale, table):
     """tir_kv_cache of tensors: k [blocks, heads, block_tokens, d] and v [blocks, heads, d, block_tokens] of torch.int8 or torch.float8_e4m3fn,
-    k_scale and v_scale [blocks, heads] float32, table [batch, columns] int32.  The operators change k, v and the scales in place; the tensors may be changed between
+    k_scale and v_scale [blocks, heads] float32, table [sequences, columns] int32.  The operators change k, v and the scales in place; the tensors may be changed between
     calls (a table's entries as blocks are handed out), but not replaced."""
     import torch
     blocks, heads, tokens, d = k.shape
@@ -63,7 +63,7 @@ def make_kv_cache(k, v, k_scale, v_scale, table):
     codes = {torch.int8: TIR_I8, torch.float8_e4m3fn: TIR_E4M3}
     if k.dtype not in codes:
         raise ValueError(f"k and v: torch.int8 or torch.float8_e4m3fn is needed, got {k.dtype}")
-    cache = KvCache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), table.data_ptr(), blocks, heads, tokens, d, table.shape[1], codes[k.dtype])
+    cache = KvCache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), table.data_ptr(), blocks, heads, tokens, d, table.shape[0], table.shape[1], codes[k.dtype])
     cache.tensors = (k, v, k_scale, v_scale, table)
     return cache
 

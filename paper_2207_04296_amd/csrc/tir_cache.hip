@@ -94,11 +94,12 @@ static tir_status check_cache(const char* who, const tir_kv_cache* c, int64_t ba
         if (c->block_tokens == (1 << s)) shift = s;
     if (!shift) return host_error(TIR_ERR_UNSUPPORTED, "%s: blocks of %lld tokens (16, 32, 64 and 128 are compiled)", who, (long long)c->block_tokens);
     if (c->blocks < 1 || c->heads < 1 || c->columns < 1) return host_error(TIR_ERR_INVALID_ARG, "%s: cache of %lld blocks, %lld heads and %lld columns: at least one of each is needed", who, (long long)c->blocks, (long long)c->heads, (long long)c->columns);
-    if (c->blocks > kMax31 || c->heads > 65535 || c->columns > (kMax31 >> shift)) return host_error(TIR_ERR_UNSUPPORTED, "%s: cache extent beyond 2^31-1 (columns * block_tokens included) or more than 65535 heads", who);
+    // (positions a few chunks behind the last one are computed with 31 bits)
+    if (c->blocks > kMax31 || c->heads > 65535 || c->columns > ((kMax31 - 65535) >> shift)) return host_error(TIR_ERR_UNSUPPORTED, "%s: blocks beyond 2^31-1, columns * block_tokens beyond 2^31-2^16 or more than 65535 heads", who);
     if (!c->k || !c->v || !c->k_scale || !c->v_scale || !c->table) return host_error(TIR_ERR_INVALID_ARG, "%s: a pointer of the cache is null", who);
     if (!host_aligned(c->k, 16) || !host_aligned(c->v, 16)) return host_error(TIR_ERR_ALIGNMENT, "%s: the cache's k and v must be 16-byte aligned", who);
     if (!host_aligned(c->k_scale, 4) || !host_aligned(c->v_scale, 4) || !host_aligned(c->table, 4)) return host_error(TIR_ERR_ALIGNMENT, "%s: the cache's scales and table must be 4-byte aligned", who);
-    (void)batch;
+    if (batch > c->sequences) return host_error(TIR_ERR_INVALID_ARG, "%s: batch of %lld, the cache's table has %lld sequences", who, (long long)batch, (long long)c->sequences);
     out->k = (char*)c->k;
     out->v = (char*)c->v;
     out->ks = c->k_scale;
@@ -194,7 +195,7 @@ tir_status tir_cache_attention(const void* Q, const tir_kv_cache* cache, void* O
 const char* tir_debug_cache_kernel(int64_t batch, int64_t T, int64_t Hq, int64_t heads, int64_t d, int64_t block_tokens, int64_t columns) {
     static thread_local char name[48];
     CacheAttnParams p = {};
-    if (batch < 1 || T < 1 || heads < 1 || Hq < heads || columns < 1) return "";
+    if (batch < 1 || T < 1 || heads < 1 || Hq < heads || columns < 1 || (d != 64 && d != 128) || (block_tokens != 16 && block_tokens != 32 && block_tokens != 64 && block_tokens != 128)) return "";
     p.batch = (int)batch;
     p.T = (int)T;
     p.G = (int)(Hq / heads);

@@ -37,7 +37,7 @@ inline tir_status check_cross(const char* who, int64_t batch, int64_t M, int64_t
     if (d != 64 && d != 128) return host_error(TIR_ERR_UNSUPPORTED, "%s: head dimension %lld (64 and 128 are compiled)", who, (long long)d);
     if (!(scale == scale) || scale > 3.0e38f || scale < -3.0e38f) return host_error(TIR_ERR_INVALID_ARG, "%s: scale must be finite", who);
     if (Hq % Hkv) return host_error(TIR_ERR_INVALID_ARG, "%s: %lld key heads do not divide %lld query heads", who, (long long)Hkv, (long long)Hq);
-    if (batch > kMax31 || M > kMax31 || N > kMax31 - 256 || Hq > kMax31) return host_error(TIR_ERR_UNSUPPORTED, "extent beyond 2^31-1");
+    if (batch > kMax31 || M > kMax31 || N > kMax31 - 65535 || Hq > kMax31) return host_error(TIR_ERR_UNSUPPORTED, "extent beyond 2^31-1");
     if (batch == 0 || Hq == 0) return TIR_OK;
     // rows of a key head, and tiles of 32 rows resp. keys of all of them
     if (M > (kMax31 - 512) / (Hq / Hkv) || batch > kMax31 / Hkv || batch * Hkv > kMax31 / ((M * (Hq / Hkv) + 31) / 32 + 1) || batch * Hkv > kMax31 / ((N + 31) / 32 + 1))

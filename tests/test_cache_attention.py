@@ -22,16 +22,16 @@ def _say(msg):
 
 # ------------------------------------------------------------------------------------------------ refusals, on the host
 def _fake_cache(**over):
-    c = dict(k=FAKE, v=FAKE, k_scale=FAKE, v_scale=FAKE, table=FAKE, blocks=4, heads=2, block_tokens=32, d=64, columns=3, dtype=B.TIR_I8)
+    c = dict(k=FAKE, v=FAKE, k_scale=FAKE, v_scale=FAKE, table=FAKE, blocks=4, heads=2, block_tokens=32, d=64, sequences=3, columns=3, dtype=B.TIR_I8)
     c.update(over)
     return B.KvCache(*[c[n] for n, _ in B.KvCache._fields_])
 
 
 CACHE_FAULTS = [
     (dict(k=0), B.TIR_ERR_INVALID_ARG), (dict(table=0), B.TIR_ERR_INVALID_ARG), (dict(v_scale=0), B.TIR_ERR_INVALID_ARG),
-    (dict(blocks=0), B.TIR_ERR_INVALID_ARG), (dict(heads=0), B.TIR_ERR_INVALID_ARG), (dict(columns=0), B.TIR_ERR_INVALID_ARG), (dict(blocks=-3), B.TIR_ERR_INVALID_ARG),
+    (dict(blocks=0), B.TIR_ERR_INVALID_ARG), (dict(heads=0), B.TIR_ERR_INVALID_ARG), (dict(columns=0), B.TIR_ERR_INVALID_ARG), (dict(blocks=-3), B.TIR_ERR_INVALID_ARG), (dict(sequences=1), B.TIR_ERR_INVALID_ARG),
     (dict(d=96), B.TIR_ERR_UNSUPPORTED), (dict(block_tokens=48), B.TIR_ERR_UNSUPPORTED), (dict(block_tokens=256), B.TIR_ERR_UNSUPPORTED), (dict(block_tokens=0), B.TIR_ERR_UNSUPPORTED),
-    (dict(dtype=B.TIR_F16), B.TIR_ERR_UNSUPPORTED), (dict(columns=2 ** 31), B.TIR_ERR_UNSUPPORTED), (dict(columns=2 ** 26), B.TIR_ERR_UNSUPPORTED), (dict(blocks=2 ** 31), B.TIR_ERR_UNSUPPORTED),
+    (dict(dtype=B.TIR_F16), B.TIR_ERR_UNSUPPORTED), (dict(columns=2 ** 31), B.TIR_ERR_UNSUPPORTED), (dict(columns=2 ** 26), B.TIR_ERR_UNSUPPORTED), (dict(columns=2 ** 26 - 2047), B.TIR_ERR_UNSUPPORTED), (dict(blocks=2 ** 31), B.TIR_ERR_UNSUPPORTED),
     (dict(k=FAKE + 8), B.TIR_ERR_ALIGNMENT), (dict(v=FAKE + 4), B.TIR_ERR_ALIGNMENT), (dict(k_scale=FAKE + 2), B.TIR_ERR_ALIGNMENT), (dict(table=FAKE + 1), B.TIR_ERR_ALIGNMENT),
 ]
 
@@ -57,7 +57,7 @@ def test_both_entry_points_reject_a_bad_cache(over, status):
 @pytest.mark.parametrize("over,status", [
     (dict(cache=None), B.TIR_ERR_INVALID_ARG), (dict(K=0), B.TIR_ERR_INVALID_ARG), (dict(V=0), B.TIR_ERR_INVALID_ARG), (dict(start=0), B.TIR_ERR_INVALID_ARG),
     (dict(batch=-1), B.TIR_ERR_INVALID_ARG), (dict(T=-1), B.TIR_ERR_INVALID_ARG), (dict(i=9), B.TIR_ERR_INVALID_ARG), (dict(k=(-640, 128, 64)), B.TIR_ERR_INVALID_ARG),
-    (dict(i="f32"), B.TIR_ERR_UNSUPPORTED), (dict(i="e4m3"), B.TIR_ERR_UNSUPPORTED), (dict(T=2 ** 31), B.TIR_ERR_UNSUPPORTED), (dict(batch=2 ** 31), B.TIR_ERR_UNSUPPORTED),
+    (dict(i="f32"), B.TIR_ERR_UNSUPPORTED), (dict(i="e4m3"), B.TIR_ERR_UNSUPPORTED), (dict(T=2 ** 31), B.TIR_ERR_UNSUPPORTED), (dict(batch=2 ** 31), B.TIR_ERR_INVALID_ARG),
     (dict(v=(2 ** 41, 128, 64)), B.TIR_ERR_UNSUPPORTED),
     (dict(K=FAKE + 2), B.TIR_ERR_ALIGNMENT), (dict(v=(640, 128, 60)), B.TIR_ERR_ALIGNMENT), (dict(start=FAKE + 2), B.TIR_ERR_ALIGNMENT), (dict(count=FAKE + 1), B.TIR_ERR_ALIGNMENT),
 ])
@@ -71,7 +71,7 @@ def test_append_rejects_bad_arguments(over, status):
     (dict(scale=float("nan")), B.TIR_ERR_INVALID_ARG), (dict(scale=float("-inf")), B.TIR_ERR_INVALID_ARG), (dict(i=-1), B.TIR_ERR_INVALID_ARG),
     (dict(o=(0, 256, 64)), B.TIR_ERR_INVALID_ARG), (dict(o=(1280, 0, 64)), B.TIR_ERR_INVALID_ARG), (dict(o=(1280, 256, 0)), B.TIR_ERR_INVALID_ARG), (dict(q=(1280, 256, -64)), B.TIR_ERR_INVALID_ARG),
     (dict(out="bf16"), B.TIR_ERR_UNSUPPORTED), (dict(i="i8", out="i32"), B.TIR_ERR_UNSUPPORTED), (dict(T=2 ** 31), B.TIR_ERR_UNSUPPORTED), (dict(T=2 ** 30, Hq=8), B.TIR_ERR_UNSUPPORTED),
-    (dict(batch=2 ** 31), B.TIR_ERR_UNSUPPORTED),
+    (dict(batch=4), B.TIR_ERR_INVALID_ARG),
     (dict(Q=FAKE + 8), B.TIR_ERR_ALIGNMENT), (dict(O=FAKE + 8), B.TIR_ERR_ALIGNMENT), (dict(o=(1280, 256, 68)), B.TIR_ERR_ALIGNMENT), (dict(lens=FAKE + 2), B.TIR_ERR_ALIGNMENT),
 ])
 def test_cache_attention_rejects_bad_arguments(over, status):
@@ -88,8 +88,8 @@ def test_make_kv_cache_checks_its_tensors():
     k, v = torch.zeros((4, 2, 32, 64), dtype=torch.int8), torch.zeros((4, 2, 64, 32), dtype=torch.int8)
     s, t = torch.zeros((4, 2)), torch.zeros((3, 5), dtype=torch.int32)
     c = B.make_kv_cache(k, v, s, s.clone(), t)
-    assert (c.blocks, c.heads, c.block_tokens, c.d, c.columns, c.dtype) == (4, 2, 32, 64, 5, B.TIR_I8)
-    assert ctypes.sizeof(B.KvCache) == 88
+    assert (c.blocks, c.heads, c.block_tokens, c.d, c.sequences, c.columns, c.dtype) == (4, 2, 32, 64, 3, 5, B.TIR_I8)
+    assert ctypes.sizeof(B.KvCache) == 96
     for bad in (dict(v=k), dict(ks=s.double()), dict(vs=s[:, :1]), dict(t=t.long()), dict(t=t[:, ::2]), dict(k=k.to(torch.uint8), v=v.to(torch.uint8)), dict(k=k.half(), v=v.half())):
         a = dict(k=k, v=v, ks=s, vs=s, t=t)
         a.update(bad)
