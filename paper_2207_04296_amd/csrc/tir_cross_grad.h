@@ -52,13 +52,16 @@ template <int DH, int RB> struct GradTile {
         const int row = wave * 8 + (lane >> 3);
         return (unsigned)(row * rs * 2 + (((lane & 7) ^ grad_swz(row)) << 4));
     }
-    static __device__ __forceinline__ void copy(char* tile, const char* base, int left, int rs, unsigned off, int wave) {
-        const int rows = left < RB ? left : RB;
+    // (rows from `left` on are zeros, whatever the stride: where it is less than a row, they would lie before the descriptor's end)
+    static __device__ __forceinline__ void copy(char* tile, const char* base, int left, int rs, unsigned off, int wave, int lane) {
+        const int rows = left < RB ? left : RB, row = wave * 8 + (lane >> 3);
         const i32x4 r = make_rsrc32(base, rows > 0 ? (unsigned)((rows - 1) * rs * 2 + ROW) : 0u);      // (rs of at most 2^23)
 #pragma unroll
-        for (int h = 0; h < HALVES; ++h)
+        for (int u = 0; u < PASSES; ++u) {
+            const unsigned at = row + u * kGradWaves * 8 < left ? off : kOutOfRange;
 #pragma unroll
-            for (int u = 0; u < PASSES; ++u) load_to_lds_at(r, tile + h * HALF + (u * kGradWaves + wave) * 1024, off, u * kGradWaves * 8 * rs * 2 + h * 128);
+            for (int h = 0; h < HALVES; ++h) load_to_lds_at(r, tile + h * HALF + (u * kGradWaves + wave) * 1024, at, u * kGradWaves * 8 * rs * 2 + h * 128);
+        }
     }
     // Operand of k-step ks (16 channels): row l31 of the 32 from row r0
     static __device__ __forceinline__ uint4 along(const char* tile, int r0, int ks, int l31, int g) {
@@ -227,8 +230,8 @@ __global__ void __launch_bounds__(kGradThreads, 2) grad_rows_kernel(const GradPa
         char* const st = smem + (i & 1) * STAGE;
         const long long key = (long long)(c0 + i) * kGradChunk;
         const int left = i < chunks ? n - (int)key : 0;
-        T::copy(st, Kb + key * k_rs * 2, left, k_rs, k_off, wave);
-        T::copy(st + T::BYTES, Vb + key * v_rs * 2, left, v_rs, v_off, wave);
+        T::copy(st, Kb + key * k_rs * 2, left, k_rs, k_off, wave, lane);
+        T::copy(st + T::BYTES, Vb + key * v_rs * 2, left, v_rs, v_off, wave, lane);
     };
     if (chunks > 0) copy(0);
 
@@ -382,8 +385,8 @@ __global__ void __launch_bounds__(kGradThreads * RG, 2) grad_keys_kernel(const G
     auto copy = [&](int st_at) __attribute__((always_inline)) {
         char* const st = ring + st_at * STAGE;
         const int hq = h * p.G + head_at, m = chunk_at * RB, left = p.M - m;
-        T::copy(st, (const char*)p.Q + 2 * (b * p.q_bs + (long long)m * q_rs + hq * p.q_hs), left, q_rs, q_off, wave);
-        T::copy(st + T::BYTES, (const char*)p.dO + 2 * (b * p.g_bs + (long long)m * go_rs + hq * p.g_hs), left, go_rs, go_off, wave);
+        T::copy(st, (const char*)p.Q + 2 * (b * p.q_bs + (long long)m * q_rs + hq * p.q_hs), left, q_rs, q_off, wave, lane);
+        T::copy(st + T::BYTES, (const char*)p.dO + 2 * (b * p.g_bs + (long long)m * go_rs + hq * p.g_hs), left, go_rs, go_off, wave, lane);
         const long long stat = ((long long)b * p.heads * p.G + hq) * p.M + m;
         // (the lanes past RB floats would write past their place)
         if (wave < 2 && lane < RB) floats_to_lds(make_rsrc32((wave ? p.delta : p.lse) + stat, (unsigned)(left < RB ? left : RB) * 4u), st + 2 * T::BYTES + wave * (RB * 4), (unsigned)lane * 4);
@@ -392,7 +395,7 @@ __global__ void __launch_bounds__(kGradThreads * RG, 2) grad_keys_kernel(const G
     };
     if (mine > 0) copy(0);
     if (V_LDS && rgrp == 0 && chunks > 0)
-        VT::copy(smem + V_AT, (const char*)p.V + 2 * (b * p.v_bs + key0 * p.v_rs + h * p.v_hs), n - key0, (int)p.v_rs, VT::lane_offset(wave, lane, (int)p.v_rs), wave);
+        VT::copy(smem + V_AT, (const char*)p.V + 2 * (b * p.v_bs + key0 * p.v_rs + h * p.v_hs), n - key0, (int)p.v_rs, VT::lane_offset(wave, lane, (int)p.v_rs), wave, lane);
 
     uint4 kf[KSTEPS], vf[V_LDS ? 1 : KSTEPS];
 #pragma unroll

@@ -307,3 +307,29 @@ def test_a_training_step_in_a_graph():
             assert torch.all((got.cpu().double() - ref[x]).abs() <= tol), (i, x)
         assert torch.isfinite(torch.randn(1 << 16, device="cuda").sum())
     B.tir_set_workspace(None, st)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+def test_strides_shorter_than_a_row(workspace, d):
+    """On the device as they are: a dO whose rows are one row, or overlap; a single query and a single key whose row strides are 0.  What is behind the last row or key is that data again and must not count."""
+    import torch
+    for m, n, q_rs, k_rs, g_rs in ((70, 90, None, None, 0), (33, 40, None, None, 8), (1, 1, 0, 0, 0), (1, 75, 0, None, 0)):
+        g = _gen(37)
+        q, kv = _inputs(g, "f16", 2, m, n, 1, 1, d, None)
+        flat = torch.randn((2, m * d + d), generator=g).to(torch.float16)
+        do = flat.as_strided((2, m, 1, d), (m * d + d, g_rs, d, 1))
+        dod = flat.cuda().as_strided(do.shape, do.stride())
+        qd, kd, vd = q.cuda(), kv[:, :, 0].contiguous().cuda(), kv[:, :, 1].contiguous().cuda()
+        o, lse, delta = torch.empty_like(qd), torch.empty((2, 1, m), device="cuda"), torch.empty((2, 1, m), device="cuda")
+        dq, dk, dv = (torch.full_like(x, MARK) for x in (qd, kd, vd))
+        rs = lambda x, r: (x.stride(0), x.stride(1) if r is None else r, x.stride(2))
+        strides = (*rs(qd, q_rs), *rs(kd, k_rs), *rs(vd, k_rs), *o.stride()[:3])
+        _say(f"short strides d={d}: {m} x {n}, {q_rs} {k_rs} {g_rs}")
+        B.tir_cross_attention(qd, kd, vd, o, lse, None, 2, m, n, 1, 1, d, *strides, 0.1, "f16", "f16")
+        B.tir_cross_attention_backward(qd, kd, vd, o, dod, lse, None, dq, dk, dv, delta, 2, m, n, 1, 1, d, *strides, *do.stride()[:3], 0.1, "f16")
+        torch.cuda.synchronize()
+        ref = R.cross_attention(q, kv[:, :, 0], kv[:, :, 1], None, 0.1, do)
+        for x, got in (("dq", dq), ("dk", dk), ("dv", dv)):
+            tol = 3 * U["f16"] * ref[x + "_sum"] + U["f16"] * ref[x].abs() + 1e-6
+            assert torch.all((got.cpu().double() - ref[x]).abs() <= tol), (x, m, n, d)
