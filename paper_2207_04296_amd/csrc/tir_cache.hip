@@ -10,6 +10,7 @@ namespace tir {
 
 template <int DT, int CT, int DH> static hipError_t launch_append_as(const AppendParams& p, int64_t batch, hipStream_t stream) {
     const dim3 grid((unsigned)(batch * p.touched * p.c.heads), 2), block(kAppendThreads);
+    if (!grid_fits(batch * p.touched * p.c.heads, kAppendThreads)) return hipErrorInvalidConfiguration;
     if (p.c.shift == 4) return launch_kernel(&cache_append_kernel<DT, CT, DH, 16>, grid, block, stream, p);
     if (p.c.shift == 5) return launch_kernel(&cache_append_kernel<DT, CT, DH, 32>, grid, block, stream, p);
     if (p.c.shift == 6) return launch_kernel(&cache_append_kernel<DT, CT, DH, 64>, grid, block, stream, p);
@@ -25,6 +26,7 @@ hipError_t launch_append(const AppendParams& p, int dt, int ct, int d, int64_t b
 
 template <int DT, int CT, int DH> static hipError_t launch_cache_as(const CacheAttnParams& p, hipStream_t stream) {
     const unsigned tiles = (unsigned)(p.batch * p.c.heads * p.tiles);
+    if (!grid_fits(tiles, p.rows_of_tile > 32 ? kCacheTileWaves * 64 : kCacheWaves * 64)) return hipErrorInvalidConfiguration;
     if (p.rows_of_tile == 16) return launch_kernel(&cache_token_kernel<DT, CT, DH>, dim3(tiles, (unsigned)p.slices), dim3(kCacheWaves * 64), stream, p);
     if (p.rows_of_tile == 32) return launch_kernel(&cache_rows_kernel<DT, CT, DH>, dim3(tiles, (unsigned)p.slices), dim3(kCacheWaves * 64), stream, p);
     constexpr int QW = kCacheTileWaves;
@@ -148,7 +150,7 @@ tir_status tir_cache_append(const tir_kv_cache* cache, const void* K, const void
     p.div_h_magic = dh.magic; p.div_h_shift = dh.shift;
     p.div_t_magic = dt.magic; p.div_t_shift = dt.shift;
     const hipError_t e = launch_append(p, (int)in, cache->dtype == TIR_I8 ? CT_I8 : CT_E4M3, (int)cache->d, batch, (hipStream_t)stream);
-    if (e != hipSuccess) return host_error(TIR_ERR_LAUNCH, "%s: launch failed: %s", who, hipGetErrorString(e));
+    if (e != hipSuccess) return launch_error(who, e);
     return TIR_OK;
 }
 
@@ -172,7 +174,7 @@ tir_status tir_cache_attention(const void* Q, const tir_kv_cache* cache, void* O
     if (!host_aligned(Q, 16) || !host_aligned(O, 16)) return host_error(TIR_ERR_ALIGNMENT, "%s: Q and O must be 16-byte aligned", who);
     if (!host_aligned(lens, 4) || !host_aligned(count, 4)) return host_error(TIR_ERR_ALIGNMENT, "%s: lens and count must be 4-byte aligned", who);
     if ((batch > 1 && o_bs == 0) || (T > 1 && o_rs == 0) || (Hq > 1 && o_hs == 0)) return host_error(TIR_ERR_INVALID_ARG, "%s: a stride of O is zero: its rows overlap", who);
-    if (T > kMax31 || Hq > kMax31 || T > (kMax31 - 64) / (Hq / p.c.heads)) return host_error(TIR_ERR_UNSUPPORTED, "extent beyond 2^31-1");
+    if (T > kMax31 || Hq > kMax31 || T > (kMax31 - 512) / (Hq / p.c.heads)) return host_error(TIR_ERR_UNSUPPORTED, "extent beyond 2^31-1");
     p.G = (int)(Hq / p.c.heads);
     p.T = (int)T;
     if (batch > kMax31 / p.c.heads || batch * p.c.heads > kMax31 / ((T * p.G + 31) / 32)) return host_error(TIR_ERR_UNSUPPORTED, "%s: too many tiles of queries", who);
@@ -188,14 +190,15 @@ tir_status tir_cache_attention(const void* Q, const tir_kv_cache* cache, void* O
     p.div_h_magic = dh.magic; p.div_h_shift = dh.shift;
     choose_cache_kernel(&p, cache->d, stream_workspace((hipStream_t)stream));
     const hipError_t e = launch_cache_attention(p, (int)in, cache->dtype == TIR_I8 ? CT_I8 : CT_E4M3, (int)cache->d, (hipStream_t)stream);
-    if (e != hipSuccess) return host_error(TIR_ERR_LAUNCH, "%s: launch failed: %s", who, hipGetErrorString(e));
+    if (e != hipSuccess) return launch_error(who, e);
     return TIR_OK;
 }
 
 const char* tir_debug_cache_kernel(int64_t batch, int64_t T, int64_t Hq, int64_t heads, int64_t d, int64_t block_tokens, int64_t columns) {
     static thread_local char name[48];
     CacheAttnParams p = {};
-    if (batch < 1 || T < 1 || heads < 1 || Hq < heads || columns < 1 || (d != 64 && d != 128) || (block_tokens != 16 && block_tokens != 32 && block_tokens != 64 && block_tokens != 128)) return "";
+    if (batch < 1 || T < 1 || heads < 1 || Hq < heads || columns < 1 || heads > 65535 || Hq > kMax31 || T > (kMax31 - 512) / (Hq / heads) || batch > kMax31 / heads ||
+        batch * heads > kMax31 / ((T * (Hq / heads) + 31) / 32) || columns > (kMax31 - 65535) / 128 || (d != 64 && d != 128) || (block_tokens != 16 && block_tokens != 32 && block_tokens != 64 && block_tokens != 128)) return "";
     p.batch = (int)batch;
     p.T = (int)T;
     p.G = (int)(Hq / heads);

@@ -14,6 +14,7 @@ template <int DT, int OUT, int DH, int QW, int KG, int KB, int FORM> static hipE
     const FastDiv dtm = make_fastdiv((unsigned)p.tiles_m);
     p.div_tm_magic = dtm.magic;
     p.div_tm_shift = dtm.shift;
+    if (!grid_fits((int64_t)p.batch * p.tiles_m, QW * KG * 64)) return hipErrorInvalidConfiguration;
     return launch_kernel(&attention_kernel<DT, OUT, DH, QW, KG, KB, FORM, CrossParams>, dim3((unsigned)(p.batch * p.tiles_m), KG > 1 ? (unsigned)p.slices : 1u), dim3(QW * KG * 64), stream, p);
 }
 
@@ -89,7 +90,7 @@ tir_status tir_cross_attention(const void* Q, const void* K, const void* V, void
     p.div_h_magic = dh.magic; p.div_h_shift = dh.shift;
     p.div_g_magic = dg.magic; p.div_g_shift = dg.shift;
     p.out32 = out == TIR_F32;
-    p.o_near = o_rs < (1 << 20) && o_hs < (1 << 28) / p.G;      // (257 * o_rs + G * o_hs + d) * 4 < 2^31
+    p.o_near = o_rs < (1 << 20) && o_hs < (1 << 28) / p.G;      // a tile's 256 rows: 255 * o_rs * 4 bytes, or with G > 1 at most 128 * o_rs * 4 + (G - 1) * o_hs * 4
     p.slices = 1;
     const StreamWorkspace ws = stream_workspace((hipStream_t)stream);
     auto share = [&](int64_t tiles, int64_t slices, int64_t most, int64_t part) {
@@ -106,14 +107,14 @@ tir_status tir_cross_attention(const void* Q, const void* K, const void* V, void
         const int64_t chunk = d == 64 ? 32 : 16;         // two per wave
         share(p.batch, 256 / p.batch, N / (8 * chunk), d == 64 ? cross_token_partial<64>(p.M) : cross_token_partial<128>(p.M));
         e = launch_cross_token(p, (int)in, (int)d, (hipStream_t)stream);
-        if (e != hipSuccess) return host_error(TIR_ERR_LAUNCH, "%s: launch failed: %s", who, hipGetErrorString(e));
+        if (e != hipSuccess) return launch_error(who, e);
         return TIR_OK;
     }
     // Few tiles of 64 rows: their keys are shared among workgroups, one of which fills a CU, as long as each of its four key groups keeps two chunks.
     const int64_t tiles = (int64_t)p.batch * ((p.M + 63) / 64), chunk = d == 64 ? 64 : 32;
     if (tiles <= 128) share(tiles, 256 / tiles, N / (8 * chunk), 2 * (d / 32 * 4096 + 512));
     e = fn(p, (hipStream_t)stream);
-    if (e != hipSuccess) return host_error(TIR_ERR_LAUNCH, "%s: launch failed: %s", who, hipGetErrorString(e));
+    if (e != hipSuccess) return launch_error(who, e);
     return TIR_OK;
 }
 

@@ -83,7 +83,7 @@ tir_status tir_cross_attention_backward(const void* Q, const void* K, const void
     p.G = (int)(Hq / Hkv);
     p.batch = (int)batch;
     p.scale = scale;
-    p.q_near = q_rs < (1 << 20) && q_hs < (1 << 28) / p.G;      // (129 * q_rs + G * q_hs + d) * 2 < 2^31
+    p.q_near = q_rs < (1 << 20) && q_hs < (1 << 28) / p.G;      // a tile's 128 rows: at most 127 * q_rs * 2 + (G - 1) * q_hs * 2 bytes
     p.scale_log2e = scale * 1.44269504088896340736f;
     const FastDiv dh = make_fastdiv((unsigned)p.heads), dg = make_fastdiv((unsigned)p.G);
     p.div_h_magic = dh.magic; p.div_h_shift = dh.shift;
@@ -97,10 +97,12 @@ tir_status tir_cross_attention_backward(const void* Q, const void* K, const void
         p.slices = slices_of(batch * Hkv * tiles, keys ? 256 : 512, steps, kGradTile * d * 4 * (keys ? 2 : 1), ws);
         return keys ? launch_grad_keys(p, (int)in, (int)d, (hipStream_t)stream) : launch_grad_rows(p, (int)in, (int)d, (hipStream_t)stream);
     };
+    const int64_t row_tiles = (M * p.G + kGradTile - 1) / kGradTile, key_tiles = (N + kGradTile - 1) / kGradTile;
+    if (!grid_fits(batch * Hkv * row_tiles, kGradThreads) || !grid_fits(batch * Hkv * key_tiles, kGradThreads)) return launch_error(who, hipErrorInvalidConfiguration);
     hipError_t e = hipSuccess;
-    if (M > 0) e = pass(false, (M * p.G + kGradTile - 1) / kGradTile, (N + kGradChunk - 1) / kGradChunk);
-    if (e == hipSuccess && N > 0) e = pass(true, (N + kGradTile - 1) / kGradTile, (M + 63) / 64 * p.G);
-    if (e != hipSuccess) return host_error(TIR_ERR_LAUNCH, "%s: launch failed: %s", who, hipGetErrorString(e));
+    if (M > 0) e = pass(false, row_tiles, (N + kGradChunk - 1) / kGradChunk);
+    if (e == hipSuccess && N > 0) e = pass(true, key_tiles, (M + 63) / 64 * p.G);
+    if (e != hipSuccess) return launch_error(who, e);
     return TIR_OK;
 }
 

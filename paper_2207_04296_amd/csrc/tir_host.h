@@ -21,6 +21,14 @@ inline bool host_aligned(const void* p, uintptr_t a) { return ((uintptr_t)p % a)
 
 constexpr int64_t kMax31 = 2147483647LL;
 
+// A launch's extent along x is counted in work items, in 32 bits.
+inline bool grid_fits(int64_t groups, int64_t threads) { return groups <= 0xffffffffll / threads; }
+// What a launcher that checks this returns, as the caller's error.
+inline tir_status launch_error(const char* who, hipError_t e) {
+    if (e == hipErrorInvalidConfiguration) return host_error(TIR_ERR_UNSUPPORTED, "%s: more workgroups than one launch can have", who);
+    return host_error(TIR_ERR_LAUNCH, "%s: launch failed: %s", who, hipGetErrorString(e));
+}
+
 // Strides of rows that the decoder's attentions read or write 16 bytes at a time.
 inline tir_status check_row_strides(const char* who, const char* what, int64_t bs, int64_t rs, int64_t hs) {
     if (bs < 0 || rs < 0 || hs < 0) return host_error(TIR_ERR_INVALID_ARG, "%s: negative stride of %s", who, what);

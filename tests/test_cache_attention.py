@@ -58,7 +58,7 @@ def test_both_entry_points_reject_a_bad_cache(over, status):
     (dict(cache=None), B.TIR_ERR_INVALID_ARG), (dict(K=0), B.TIR_ERR_INVALID_ARG), (dict(V=0), B.TIR_ERR_INVALID_ARG), (dict(start=0), B.TIR_ERR_INVALID_ARG),
     (dict(batch=-1), B.TIR_ERR_INVALID_ARG), (dict(T=-1), B.TIR_ERR_INVALID_ARG), (dict(i=9), B.TIR_ERR_INVALID_ARG), (dict(k=(-640, 128, 64)), B.TIR_ERR_INVALID_ARG),
     (dict(i="f32"), B.TIR_ERR_UNSUPPORTED), (dict(i="e4m3"), B.TIR_ERR_UNSUPPORTED), (dict(T=2 ** 31), B.TIR_ERR_UNSUPPORTED), (dict(batch=2 ** 31), B.TIR_ERR_INVALID_ARG),
-    (dict(v=(2 ** 41, 128, 64)), B.TIR_ERR_UNSUPPORTED),
+    (dict(v=(2 ** 41, 128, 64)), B.TIR_ERR_UNSUPPORTED), (dict(batch=2 ** 23, cache=_fake_cache(sequences=2 ** 23)), B.TIR_ERR_UNSUPPORTED),
     (dict(K=FAKE + 2), B.TIR_ERR_ALIGNMENT), (dict(v=(640, 128, 60)), B.TIR_ERR_ALIGNMENT), (dict(start=FAKE + 2), B.TIR_ERR_ALIGNMENT), (dict(count=FAKE + 1), B.TIR_ERR_ALIGNMENT),
 ])
 def test_append_rejects_bad_arguments(over, status):
@@ -71,7 +71,7 @@ def test_append_rejects_bad_arguments(over, status):
     (dict(scale=float("nan")), B.TIR_ERR_INVALID_ARG), (dict(scale=float("-inf")), B.TIR_ERR_INVALID_ARG), (dict(i=-1), B.TIR_ERR_INVALID_ARG),
     (dict(o=(0, 256, 64)), B.TIR_ERR_INVALID_ARG), (dict(o=(1280, 0, 64)), B.TIR_ERR_INVALID_ARG), (dict(o=(1280, 256, 0)), B.TIR_ERR_INVALID_ARG), (dict(q=(1280, 256, -64)), B.TIR_ERR_INVALID_ARG),
     (dict(out="bf16"), B.TIR_ERR_UNSUPPORTED), (dict(i="i8", out="i32"), B.TIR_ERR_UNSUPPORTED), (dict(T=2 ** 31), B.TIR_ERR_UNSUPPORTED), (dict(T=2 ** 30, Hq=8), B.TIR_ERR_UNSUPPORTED),
-    (dict(batch=4), B.TIR_ERR_INVALID_ARG),
+    (dict(batch=4), B.TIR_ERR_INVALID_ARG), (dict(batch=2 ** 24, cache=_fake_cache(sequences=2 ** 24)), B.TIR_ERR_UNSUPPORTED),
     (dict(Q=FAKE + 8), B.TIR_ERR_ALIGNMENT), (dict(O=FAKE + 8), B.TIR_ERR_ALIGNMENT), (dict(o=(1280, 256, 68)), B.TIR_ERR_ALIGNMENT), (dict(lens=FAKE + 2), B.TIR_ERR_ALIGNMENT),
 ])
 def test_cache_attention_rejects_bad_arguments(over, status):
@@ -332,6 +332,8 @@ def test_the_tall_calls_take_the_tall_tiles():
     assert B.tir_debug_cache_kernel(64, 1, 32, 8, 128, 64, 128) == "rows16/z1"
     assert B.tir_debug_cache_kernel(1, 1, 32, 8, 128, 128, 1563) == "rows16/z32"
     assert B.tir_debug_cache_kernel(2, 5, 16, 4, 64, 16, 100) == "rows32/z7" and B.tir_debug_cache_kernel(2, 4, 16, 4, 64, 16, 100) == "rows16/z4"
+    for beyond in ((2 ** 32, 1, 8, 8, 64, 16, 5), (1, 2 ** 31, 8, 8, 64, 16, 5), (1, 1, 2 ** 33, 2 ** 32, 64, 16, 5), (1, 1, 8, 8, 64, 16, 2 ** 32), (2 ** 30, 2 ** 20, 8, 8, 64, 16, 5)):
+        assert B.tir_debug_cache_kernel(*beyond) == ""
 
 
 @pytest.mark.gpu

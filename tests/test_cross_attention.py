@@ -38,6 +38,8 @@ FAULTS = [
     (dict(d=80), B.TIR_ERR_UNSUPPORTED), (dict(i="i8"), B.TIR_ERR_UNSUPPORTED),
     (dict(M=2 ** 31), B.TIR_ERR_UNSUPPORTED), (dict(N=2 ** 31), B.TIR_ERR_UNSUPPORTED), (dict(M=2 ** 30, Hq=8, Hkv=1), B.TIR_ERR_UNSUPPORTED), (dict(batch=2 ** 30, M=200), B.TIR_ERR_UNSUPPORTED),
     (dict(k=(896, 2 ** 24, 64)), B.TIR_ERR_UNSUPPORTED),
+    # more workgroups than a launch has room for: few rows, and many
+    (dict(batch=2 ** 24, M=1, N=1), B.TIR_ERR_UNSUPPORTED), (dict(batch=2 ** 23, M=200, N=1), B.TIR_ERR_UNSUPPORTED),
     (dict(Q=FAKE + 8), B.TIR_ERR_ALIGNMENT), (dict(K=FAKE + 2), B.TIR_ERR_ALIGNMENT), (dict(v=(896, 132, 64)), B.TIR_ERR_ALIGNMENT), (dict(lens=FAKE + 2), B.TIR_ERR_ALIGNMENT), (dict(lse=FAKE + 1), B.TIR_ERR_ALIGNMENT),
 ]
 
