@@ -333,15 +333,16 @@ __global__ void __launch_bounds__(kGradThreads, 2) grad_rows_kernel(const GradPa
 // RG = 2: two groups of four waves on the same keys, which take every other chunk of rows through a ring each and are added through LDS at the end: two waves per SIMD where there is
 // one workgroup per CU.
 // A block's phases run one after the other (S and P, dV, dP and dS, dK): at d = 128 sums and keys are 160 registers, and 256 hold two waves per SIMD.  The values would be 32 more: there
-// they stay in LDS.
+// they stay in LDS, and so they do at d = 64 with RG = 1, where 168 registers then hold three workgroups per CU instead of two: 16 x 250 x 333 x 12 heads (576 workgroups) both passes 41.0 -> 37.3 us,
+// 4 x 4096 x 577 x 8 heads 119 -> 114.
 // ---------------------------------------------------------------------------------------------
 template <int DT, int DH, int RG>
-__global__ void __launch_bounds__(kGradThreads * RG, 2) grad_keys_kernel(const GradParams p) {
+__global__ void __launch_bounds__(kGradThreads * RG, DH == 64 && RG == 1 ? 3 : 2) grad_keys_kernel(const GradParams p) {
     constexpr int RB = DH == 64 ? 64 : 32;              // rows of a chunk
     typedef GradTile<DH, RB> T;
     constexpr int KSTEPS = DH / 16, DB = DH / 32, STAGE = 2 * T::BYTES + 2 * RB * 4, MERGE = 2 * DB * 4096;      // (MERGE: a wave's sums)
-    constexpr int LA = 3;
-    constexpr bool V_LDS = DH == 128;
+    constexpr int LA = DH == 64 && RG == 1 ? 2 : 3;
+    constexpr bool V_LDS = DH == 128 || RG == 1;
     typedef GradTile<DH, kGradTile> VT;
     constexpr int V_AT = RG * 2 * STAGE, USED = V_AT + (V_LDS ? VT::BYTES : 0);
     constexpr int LDS = USED > (RG - 1) * kGradWaves * MERGE ? USED : (RG - 1) * kGradWaves * MERGE;
