@@ -11,19 +11,24 @@
  *                                        * W[co, rh, rw, rc]                   (sec. 4.2 Conv2D formula;
  *                       mapped onto Eq. 1 by ReIndex + fuse: x = fuse(n,h,w), y = co, k = fuse(rh,rw,rc))
  *
+ * and attention, which is two of them with a softmax in between: over dense heads (tir_attention), over a cache of keys
+ * and values in 8 bits (tir_cache_append, tir_cache_attention) and over another sequence's states, with its gradients
+ * (tir_cross_attention, tir_cross_attention_backward).
+ *
  * Common conventions
  *   - Every pointer is a DEVICE pointer owned by the caller.  The operator entry points never allocate or free
  *     device memory, never copy to the host and never synchronise: each call enqueues kernels on `stream` and
  *     returns, also while `stream` (or any other stream) is being captured.  The only calls that block or create
  *     HIP objects are the tuning calls (tir_tune_*), which say so.
- *   - One kernel path needs scratch memory: a reduction that is split over several workgroups per output tile
+ *   - Some kernels need scratch memory: a reduction that is split over several workgroups per output tile
  *     (few small tiles facing a long K; the variant queries report it as "<variant>/z<slices>") keeps partial sums
  *     and arrival counters in a workspace.  The library owns none: it plans such a split only for launches on a
  *     stream for which the caller has registered a buffer (tir_set_workspace), and plans the same problem
  *     unsplit otherwise.  The result does not depend on the split's timing: the partial sums are added in a
- *     fixed order.  tir_gemm_split_static is the variant for callers that cannot provide a buffer either.
+ *     fixed order.  tir_gemm_split_static is the variant for callers that cannot provide a buffer either.  The attentions
+ *     over a cache and over another sequence, and their gradients, share keys or rows among workgroups in the same way.
  *   - The output is fully overwritten (reduction init is 0; there is no alpha / beta), and must not
- *     overlap an input.
+ *     overlap an input.  The operators on a cache say what they leave as it was.
  *   - Inputs F16 / BF16 accumulate in fp32; input I8 accumulates in int32 (wrap-around on overflow,
  *     which inputs in [-127,127] with K <= 133000 cannot reach).
  *   - Allowed (in, out) pairs: (F16, F32) (F16, F16) (BF16, F32) (BF16, BF16) (I8, I32).
@@ -49,7 +54,7 @@ typedef enum {
     TIR_OK = 0,
     TIR_ERR_INVALID_ARG = 1,  /* null pointer, negative size or stride, bad dtype code, groups not dividing */
     TIR_ERR_UNSUPPORTED = 2,  /* a (in, out) dtype pair outside the list above, or sizes beyond 2^31-1 */
-    TIR_ERR_ALIGNMENT = 3,    /* pointer not aligned to its element size */
+    TIR_ERR_ALIGNMENT = 3,    /* pointer not aligned to its element size (attention: pointers and strides to 16 bytes) */
     TIR_ERR_LAUNCH = 4        /* the HIP runtime refused the launch; message holds hipGetErrorString */
 } tir_status;
 
