@@ -299,7 +299,8 @@ const char* tir_last_error(void);
  * captured from `stream` keeps using it: two graphs that may run at the same time are captured from streams with
  * buffers of their own);
  * ws = NULL removes the registration (later launches on `stream` run unsplit).  Two streams that may run at the
- * same time need two buffers: launches that share one race.  Tuning calls use the workspace of the stream they
+ * same time need two buffers: launches that share one race.  Operators that threads call on one stream take turns at
+ * its buffer.  Tuning calls use the workspace of the stream they
  * are given and try split reductions only if it has one.
  * Errors: TIR_ERR_INVALID_ARG (buffer too small), TIR_ERR_ALIGNMENT, TIR_ERR_LAUNCH; the previous
  * registration stays in place then.

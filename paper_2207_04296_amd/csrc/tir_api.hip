@@ -226,6 +226,7 @@ static const int64_t kWsTiles = 16384;           // ... and its counters
 struct Workspace {
     void* partial;
     unsigned* count;
+    std::shared_ptr<std::mutex> turn;            // held over the launches of an operator that uses it
 };
 static std::mutex g_ws_mu;
 static std::map<std::pair<int, hipStream_t>, Workspace> g_ws;
@@ -273,16 +274,29 @@ static SplitLimits stream_split_limits(hipStream_t stream) {
 }
 
 StreamWorkspace stream_workspace(hipStream_t stream) {
-    const StreamWorkspace none = {nullptr, nullptr, 0, 0};
-    if (!g_any_ws.load(std::memory_order_acquire)) return none;
+    StreamWorkspace ws = {};
+    if (!g_any_ws.load(std::memory_order_acquire)) return ws;
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess) {
         (void)hipGetLastError();
-        return none;
+        return ws;
     }
-    std::lock_guard<std::mutex> lock(g_ws_mu);
-    auto it = g_ws.find(std::make_pair(dev, stream));
-    return it == g_ws.end() ? none : StreamWorkspace{it->second.partial, it->second.count, kWsBytes, kWsTiles};
+    for (;;) {
+        {
+            std::lock_guard<std::mutex> lock(g_ws_mu);
+            auto it = g_ws.find(std::make_pair(dev, stream));
+            if (it == g_ws.end()) return StreamWorkspace{};
+            if (ws.turn.owns_lock() && it->second.turn == ws.mutex) return ws;      // (and not replaced while this thread waited)
+            if (ws.turn.owns_lock()) ws.turn.unlock();
+            ws.turn = std::unique_lock<std::mutex>();
+            ws.partial = it->second.partial;
+            ws.count = it->second.count;
+            ws.bytes = kWsBytes;
+            ws.counters = kWsTiles;
+            ws.mutex = it->second.turn;
+        }
+        ws.turn = std::unique_lock<std::mutex>(*ws.mutex);
+    }
 }
 
 // The kernels divide by these launch constants through multiply-and-shift (see Params); a GEMM divides by one of them.
@@ -982,7 +996,8 @@ static tir_status plan_conv(bool need_ptrs, const void* x, const void* w, void* 
 
 // Give a plan with a split reduction the workspace registered for its stream (the plan was made with that stream's
 // limits; should the registration have gone meanwhile, the same variant runs unsplit).
-static tir_status attach_workspace(Plan* plan, hipStream_t stream) {
+static tir_status attach_workspace(Plan* plan, hipStream_t stream, StreamWorkspace* held = nullptr) {
+    if (held && plan->v && plan->p.ksplit > 1) *held = stream_workspace(stream);
     if (!plan->v || plan->p.ksplit <= 1) return TIR_OK;
     int dev = 0;
     hipError_t e = hipGetDevice(&dev);
@@ -1019,7 +1034,8 @@ static tir_status run(const Plan& plan, hipStream_t stream) {
 }
 
 static tir_status launch(Plan& plan, hipStream_t stream) {
-    tir_status st = attach_workspace(&plan, stream);
+    StreamWorkspace held = {};
+    tir_status st = attach_workspace(&plan, stream, &held);
     if (st != TIR_OK) return st;
     return run(plan, stream);
 }
@@ -1324,7 +1340,7 @@ tir_status tir_set_workspace(tir_stream stream_, void* ws, uint64_t bytes) {
     hipLaunchKernelGGL(clear_counters_kernel, dim3((unsigned)(kWsTiles / 256)), dim3(256), 0, stream, count, (int)kWsTiles);
     e = hipGetLastError();
     if (e != hipSuccess) return fail(TIR_ERR_LAUNCH, "clearing the workspace counters failed: %s", hipGetErrorString(e));
-    g_ws[key] = Workspace{ws, count};
+    g_ws[key] = Workspace{ws, count, std::make_shared<std::mutex>()};
     g_any_ws.store(true, std::memory_order_release);
     return TIR_OK;
 }

@@ -1,6 +1,8 @@
 // What the entry points of the other translation units share with tir_api.hip: error reports and the workspace a caller registered.
 #pragma once
 #include <hip/hip_runtime.h>
+#include <memory>
+#include <mutex>
 #include "tir.h"
 
 namespace tir {
@@ -9,11 +11,14 @@ namespace tir {
 tir_status host_error(tir_status st, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
 
 // The workspace registered for `stream` of the current device (tir_set_workspace): partial sums and zeroed arrival counters.  partial is
-// null where there is none: what needs it runs unsplit then.
+// null where there is none: what needs it runs unsplit then.  While the object lives, no other thread's call launches anything that uses this workspace: an operator may be several launches that
+// pass results through it.
 struct StreamWorkspace {
     void* partial;
     unsigned* count;
     int64_t bytes, counters;
+    std::shared_ptr<std::mutex> mutex;
+    std::unique_lock<std::mutex> turn;
 };
 StreamWorkspace stream_workspace(hipStream_t stream);
 

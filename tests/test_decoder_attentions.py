@@ -113,3 +113,68 @@ def test_a_decoder_layer_serves_prompts_and_tokens(dtype, cache, group):
     finally:
         torch.cuda.synchronize()
         B.tir_set_workspace(None)
+
+
+@pytest.mark.gpu
+def test_threads_that_call_on_one_stream_take_turns():
+    """Gradients and an attention whose partial results pass from one launch to the next, and a product with a split reduction, called by three threads on one stream: as when called alone, to the bit."""
+    import threading
+
+    import torch
+    g = torch.Generator().manual_seed(5)
+    m, n, d = 1500, 77, 64
+    q, k, v, do = (torch.randn((1, x, 2, d), generator=g).to(torch.bfloat16).cuda() for x in (m, n, n, m))
+    o, lse = torch.empty_like(q), torch.empty((1, 2, m), device="cuda")
+    a, b = (torch.randn((64, 8192), generator=g).to(torch.bfloat16).cuda() for _ in range(2))
+    heads, bt, length, T = 4, 64, 5001, 130                       # (256-row tiles, sliced)
+    cols = -(-length // bt)
+    pool = [torch.randint(-100, 100, s, generator=g).to(torch.int8).cuda() for s in ((cols, heads, bt, d), (cols, heads, d, bt))]
+    cache = B.make_kv_cache(*pool, *(torch.full((cols, heads), 0.01, device="cuda") for _ in range(2)), torch.arange(cols, dtype=torch.int32, device="cuda")[None])
+    cq = torch.randn((1, T, 4 * heads, d), generator=g).to(torch.bfloat16).cuda()
+    lens = torch.tensor([length], dtype=torch.int32, device="cuda")
+    st = torch.cuda.Stream()
+    ws = torch.empty(B.tir_workspace_bytes(), dtype=torch.uint8, device="cuda")
+    strides = (*q.stride()[:3], *k.stride()[:3], *v.stride()[:3], *o.stride()[:3])
+    assert B.tir_debug_cache_kernel(1, T, 4 * heads, heads, d, bt, cols) == "rows256/z19"
+    assert "/z" in B.tir_gemm_variant(1, 64, 64, 8192, 8192, 1, 1, 8192, 64, 1, "bf16", "f32")
+
+    def backward():
+        dq, dk, dv = (torch.empty_like(x) for x in (q, k, v))
+        delta = torch.empty_like(lse)
+        B.tir_cross_attention_backward(q, k, v, o, do, lse, None, dq, dk, dv, delta, 1, m, n, 2, 2, d, *strides, *do.stride()[:3], 0.1, "bf16", st)
+        return dq, dk, dv
+
+    def attend():
+        out = torch.empty_like(cq)
+        B.tir_cache_attention(cq, cache, out, lens, None, 1, T, 4 * heads, *cq.stride()[:3], *out.stride()[:3], 0.1, "bf16", "bf16", st)
+        return (out,)
+
+    def product():
+        c = torch.empty((64, 64), device="cuda")
+        B.tir_gemm(a, b, c, 64, 64, 8192, 8192, 1, 1, 8192, 64, 1, "bf16", "f32", st)
+        return (c,)
+    torch.cuda.synchronize()
+    B.tir_set_workspace(ws, st)
+    try:
+        B.tir_cross_attention(q, k, v, o, lse, None, 1, m, n, 2, 2, d, *strides, 0.1, "bf16", "bf16", st)
+        calls = (backward, attend, product)
+        alone = [f() for f in calls]
+        torch.cuda.synchronize()
+        results = [[] for _ in calls]
+
+        def work(i):
+            with torch.cuda.stream(st):
+                for _ in range(40):
+                    results[i].append(calls[i]())
+        threads = [threading.Thread(target=work, args=(i,)) for i in range(len(calls))]
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join(60)
+        torch.cuda.synchronize()
+        print("[case] three threads on one stream", flush=True)
+        for want, got in zip(alone, results):
+            assert len(got) == 40 and all(torch.equal(x, y) for r in got for x, y in zip(want, r))
+    finally:
+        torch.cuda.synchronize()
+        B.tir_set_workspace(None, st)
