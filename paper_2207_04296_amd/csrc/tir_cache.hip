@@ -188,7 +188,8 @@ tir_status tir_cache_attention(const void* Q, const tir_kv_cache* cache, void* O
     const FastDiv dg = make_fastdiv((unsigned)p.G), dh = make_fastdiv((unsigned)p.c.heads);
     p.div_g_magic = dg.magic; p.div_g_shift = dg.shift;
     p.div_h_magic = dh.magic; p.div_h_shift = dh.shift;
-    choose_cache_kernel(&p, cache->d, stream_workspace((hipStream_t)stream));
+    const StreamWorkspace ws = stream_workspace((hipStream_t)stream);
+    choose_cache_kernel(&p, cache->d, ws);
     const hipError_t e = launch_cache_attention(p, (int)in, cache->dtype == TIR_I8 ? CT_I8 : CT_E4M3, (int)cache->d, (hipStream_t)stream);
     if (e != hipSuccess) return launch_error(who, e);
     return TIR_OK;
