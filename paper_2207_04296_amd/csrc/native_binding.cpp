@@ -7,7 +7,7 @@
 //
 // Conversions by C parameter type: pointers take a tensor (its data_ptr()), an integer address or None; tir_dtype a
 // code or a name ("f16", ...); const tir_epilogue* None or an instance of the binding's Epilogue (set_epilogue_type), const tir_kv_cache* an instance of
-// its KvCache (set_cache_type); the last argument, the
+// its KvCache (set_cache_type); int32_t* and float* take a dense device tensor of that type (lengths are int64 by torch's default, and would be read as pairs), an address or None; the last argument, the
 // stream, None (torch's current stream), an integer handle or an object with .cuda_stream.  Every function returns the
 // tir_status as an int; wrong argument types raise.
 #define PY_SSIZE_T_CLEAN
@@ -24,6 +24,11 @@ namespace {
 
 PyObject* g_data_ptr = nullptr;       // interned method / attribute names
 PyObject* g_cuda_stream = nullptr;
+PyObject* g_dtype = nullptr;
+PyObject* g_is_cuda = nullptr;
+PyObject* g_is_contiguous = nullptr;
+PyObject* g_int32 = nullptr;          // torch.int32, torch.float32
+PyObject* g_float32 = nullptr;
 PyObject* g_current_stream = nullptr; // torch.cuda.current_stream: initialises the device, used for the first None
 PyObject* g_get_device = nullptr;     // torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 PyObject* g_raw_stream = nullptr;
@@ -45,6 +50,23 @@ bool to_address(PyObject* o, void** out) {
     *out = PyLong_AsVoidPtr(r);
     Py_DECREF(r);
     return !(*out == nullptr && PyErr_Occurred());
+}
+
+bool to_array(PyObject* o, void** out, PyObject* type, const char* name) {
+    if (o == Py_None || PyLong_Check(o)) return to_address(o, out);
+    PyObject* const t = PyObject_GetAttr(o, g_dtype);
+    PyObject* const cuda = t ? PyObject_GetAttr(o, g_is_cuda) : nullptr;
+    PyObject* const dense = cuda ? PyObject_CallMethodNoArgs(o, g_is_contiguous) : nullptr;
+    const bool known = dense != nullptr, fits = t == type && cuda == Py_True && dense == Py_True;
+    Py_XDECREF(t);
+    Py_XDECREF(cuda);
+    Py_XDECREF(dense);
+    if (!known) return false;
+    if (!fits) {
+        PyErr_Format(PyExc_TypeError, "expected a dense %s tensor on the device, its address or None", name);
+        return false;
+    }
+    return to_address(o, out);
 }
 
 bool to_stream(PyObject* o, void** out) {
@@ -140,9 +162,9 @@ template <class S> bool convert_struct(PyObject* o, const S** out, Held& h, PyOb
 }
 bool convert(PyObject* o, const tir_epilogue** out, Held& h) { return convert_struct(o, out, h, g_epilogue_type, "epilogue", "Epilogue"); }
 bool convert(PyObject* o, const tir_kv_cache** out, Held& h) { return convert_struct(o, out, h, g_cache_type, "cache", "instance of KvCache"); }
-bool convert(PyObject* o, const int32_t** out, Held&) { return to_address(o, (void**)out); }
-bool convert(PyObject* o, float** out, Held&) { return to_address(o, (void**)out); }
-bool convert(PyObject* o, const float** out, Held&) { return to_address(o, (void**)out); }
+bool convert(PyObject* o, const int32_t** out, Held&) { return to_array(o, (void**)out, g_int32, "int32"); }
+bool convert(PyObject* o, float** out, Held&) { return to_array(o, (void**)out, g_float32, "float32"); }
+bool convert(PyObject* o, const float** out, Held&) { return to_array(o, (void**)out, g_float32, "float32"); }
 
 template <class... A, size_t... I>
 PyObject* invoke(tir_status (*fn)(A...), PyObject* const* args, std::index_sequence<I...>) {
@@ -221,6 +243,11 @@ PyMODINIT_FUNC PyInit__native(void) {
     g_current_stream = attribute("torch.cuda", "current_stream");
     if (g_current_stream) g_get_device = attribute("torch._C", "_cuda_getDevice");
     if (g_get_device) g_raw_stream = attribute("torch._C", "_cuda_getCurrentRawStream");
-    if (!g_data_ptr || !g_cuda_stream || !g_raw_stream) return nullptr;
+    g_dtype = PyUnicode_InternFromString("dtype");
+    g_is_cuda = PyUnicode_InternFromString("is_cuda");
+    g_is_contiguous = PyUnicode_InternFromString("is_contiguous");
+    if (g_raw_stream) g_int32 = attribute("torch", "int32");
+    if (g_int32) g_float32 = attribute("torch", "float32");
+    if (!g_data_ptr || !g_cuda_stream || !g_raw_stream || !g_dtype || !g_is_cuda || !g_is_contiguous || !g_float32) return nullptr;
     return PyModule_Create(&kModule);
 }

@@ -178,3 +178,26 @@ def test_threads_that_call_on_one_stream_take_turns():
     finally:
         torch.cuda.synchronize()
         B.tir_set_workspace(None, st)
+
+
+def test_the_binding_wants_lengths_and_statistics_as_they_are_read():
+    """int64 (torch's default), host, or strided arrays of lengths, and other statistics than fp32 ones, are refused before anything is launched."""
+    import torch
+    assert B._load_native()
+    x, wrong = 4096, [torch.tensor([1, 2]), torch.tensor([1, 2], dtype=torch.int32), torch.zeros(4, dtype=torch.int32)[::2]]
+    cache = B.KvCache(x, x, x, x, x, 4, 2, 32, 64, 2, 3, B.TIR_I8)
+    s = (640, 128, 64)
+    for bad in wrong:
+        for start, count in ((bad, None), (x, bad)):
+            with pytest.raises(TypeError, match="int32"):
+                B.tir_cache_append(cache, x, x, start, count, 2, 1, *s, *s, "f16", 0)
+            with pytest.raises(TypeError, match="int32"):
+                B.tir_cache_attention(x, cache, x, start, count, 2, 1, 2, *s, *s, 0.1, "f16", "f16", 0)
+        with pytest.raises(TypeError, match="int32"):
+            B.tir_cross_attention(x, x, x, x, None, bad, 2, 1, 3, 2, 2, 64, *s, *s, *s, *s, 0.1, "f16", "f16", 0)
+    for bad in (torch.zeros(2, 2, 1), torch.zeros(2, 2, 1, dtype=torch.float64)):
+        with pytest.raises(TypeError, match="float32"):
+            B.tir_cross_attention(x, x, x, x, bad, None, 2, 1, 3, 2, 2, 64, *s, *s, *s, *s, 0.1, "f16", "f16", 0)
+        for lse, delta in ((bad, x), (x, bad)):
+            with pytest.raises(TypeError, match="float32"):
+                B.tir_cross_attention_backward(x, x, x, x, x, lse, None, x, x, x, delta, 2, 1, 3, 2, 2, 64, *s, *s, *s, *s, *s, 0.1, "f16", 0)
