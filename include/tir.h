@@ -270,7 +270,8 @@ tir_status tir_cross_attention(const void* Q, const void* K, const void* V, void
  *     dV_j = sum_i P_ij dO_i     dS_ij = P_ij (dO_i . V_j - D_i)     dQ_i = scale * sum_j dS_ij K_j     dK_j = scale * sum_i dS_ij Q_i
  * the sums of dK and dV running over all query heads that share the key head as well.  dQ has Q's type and strides, dK and dV those of K and V; they are fully overwritten: rows of dK and
  * dV from lens[b] on are zeros, as are the rows of dQ of a sequence without keys.  A stride of Q, K or V that is 0 along an axis of more than one is refused: the gradients would overlap
- * (the gradient of a broadcast input is the sum over what it was broadcast to); other strides have to keep their rows apart, those of O and dO may be 0.  delta: scratch of the caller's, fp32 [batch][Hq][M]; holds D afterwards.
+ * (the gradient of a broadcast input is the sum over what it was broadcast to); other strides have to keep their rows apart, those of O and dO may be 0.  delta: scratch of the caller's, fp32 [batch][Hq][M]; holds D afterwards
+ * (of sequences of up to 64 keys summed from P and dO . V, which O's rounding does not reach).
  * Nothing is added atomically: the same call gives the same bits.  P and dS are rounded to the input type for the last products (F16: times a power of two that uses the type's range), sums are fp32.
  * With a workspace registered for `stream` few rows, or few keys, are shared among workgroups.
  * Conventions of pointers and strides as in the forward call; no tensor may overlap an output.  batch or Hq = 0 is a no-op.

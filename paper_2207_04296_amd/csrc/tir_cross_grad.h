@@ -239,6 +239,10 @@ __global__ void __launch_bounds__(kGradThreads, 2) grad_rows_kernel(const GradPa
     const int row = row0 + wave * 32 + l31;
     const bool live = wave * 32 + l31 < rows;
     const int m = (int)fastdiv((unsigned)row, p.div_g_magic, p.div_g_shift), hq = h * p.G + row - m * p.G;
+    // D = dO . O, but of a sequence of one chunk sum_j P dP, whose terms are all at hand: O was rounded, and where few keys share a row's weight that error is as large as what dP - D leaves
+    // (5 keys, bf16: dQ and dK
+    // off by 2.77e-3 relative in the mean, and this way by 2.36e-3, which is the rounding of dS and of the result).  O is not read then: 3 x 2500 x 19 keys x 56 query heads of 128 172 -> 152 us.
+    const bool few = n <= kGradChunk;
     uint4 qf[KSTEPS], of[KSTEPS];
     float delta = 0.f, lse2 = 0.f;
     const long long stat = ((long long)b * p.heads * p.G + hq) * p.M + m;
@@ -252,9 +256,23 @@ __global__ void __launch_bounds__(kGradThreads, 2) grad_rows_kernel(const GradPa
         for (int ks = 0; ks < KSTEPS; ++ks) {
             qf[ks] = *(const uint4*)(q + ks * 32);
             of[ks] = *(const uint4*)(go + ks * 32);
-            delta += dot8<DT>(of[ks], *(const uint4*)(o + ks * 32));
+            if (!few) delta += dot8<DT>(of[ks], *(const uint4*)(o + ks * 32));
         }
         lse2 = p.lse[stat] * 1.44269504088896340736f;
+    }
+    const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (few && chunks > 0) {
+        copy_barrier<0>();
+#pragma unroll 1
+        for (int jb = 0; jb * 32 < n; ++jb) {
+            f32x16 s, dp;
+#pragma unroll
+            for (int ks = 0; ks < KSTEPS; ++ks) s = InTraits<DT>::mfma(T::along(smem, jb * 32, ks, l31, g), qf[ks], ks == 0 ? zero16 : s);
+#pragma unroll
+            for (int ks = 0; ks < KSTEPS; ++ks) dp = InTraits<DT>::mfma(T::along(smem + T::BYTES, jb * 32, ks, l31, g), of[ks], ks == 0 ? zero16 : dp);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) delta += jb * 32 + 8 * (r >> 2) + 4 * g + (r & 3) < n ? __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], p.scale_log2e, -lse2)) * dp[r] : 0.f;
+        }
     }
     delta += __shfl_xor(delta, 32);
     if (live && g == 0 && blockIdx.y == 0) p.delta[stat] = delta;
@@ -265,7 +283,6 @@ __global__ void __launch_bounds__(kGradThreads, 2) grad_rows_kernel(const GradPa
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[db][r] = 0.f;
     float by = DT == DT_F16 ? kFirstFactor : 1.f;
-    const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 
     for (int i = 0; i < chunks; ++i) {
         copy_barrier<0>();                     // chunk i is in, and everybody is past chunk i - 1

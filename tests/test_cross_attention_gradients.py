@@ -333,3 +333,30 @@ def test_strides_shorter_than_a_row(workspace, d):
         for x, got in (("dq", dq), ("dk", dk), ("dv", dv)):
             tol = 3 * U["f16"] * ref[x + "_sum"] + U["f16"] * ref[x].abs() + 1e-6
             assert torch.all((got.cpu().double() - ref[x]).abs() <= tol), (x, m, n, d)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("f16", 64), ("f16", 128)])
+def test_few_keys_with_nearly_the_same_values(workspace, dtype, d):
+    """Values 8 and a tenth around it: dP - D is a hundredth of either, and an O that was rounded would be seen in D.  Per element: dS is rounded once, the result once, and dP and D are fp32 sums of d
+    resp. n terms: 2^-24 * (d + 64 + 64) <= 2e-5 of sum_c |dO| |V| each, so |error| <= u * sum |dS| |K| * 1.01 + 4e-5 * sum P (|dO| |V|) |K| + u * |ref| (dK alike)."""
+    import torch
+    g = _gen(41)
+    batch, m, n, scale, u = 3, 50, 60, 0.125, U[dtype]
+    t = R.TORCH[dtype]
+    lens = [60, 33, 5]
+    q, k, do = (torch.randn((batch, x, 2, d), generator=g).to(t) for x in (m, n, m))
+    v = (8 + 0.1 * torch.randn((batch, n, 2, d), generator=g)).to(t)
+    got = _forward_and_backward(q, torch.stack((k, v), 2), do, lens, scale, dtype)
+    worst = 0.0
+    for b, length in enumerate(lens):
+        Q, K, V, G = (x[b, :y].double().transpose(0, 1) for x, y in ((q, m), (k, length), (v, length), (do, m)))
+        P = torch.softmax(scale * Q @ K.transpose(1, 2), -1)
+        dP = G @ V.transpose(1, 2)
+        dS = P * (dP - (P * dP).sum(-1, keepdim=True))
+        fuzz = 4e-5 * P * (G.abs() @ V.abs().transpose(1, 2)) + 1.01 * u * dS.abs()
+        for name, ref, mag, out in (("dq", dS @ K, fuzz @ K.abs(), got["dq"][b]), ("dk", dS.transpose(1, 2) @ Q, fuzz.transpose(1, 2) @ Q.abs(), got["dk"][b, :length])):
+            ref, mag = scale * ref.transpose(0, 1), scale * mag.transpose(0, 1)
+            worst = max(worst, float(((out.double() - ref).abs() / (mag + u * ref.abs() + 2.0 ** -25)).max()))
+    _say(f"few keys, near values, {dtype} d={d}: {worst:.3g} of the tolerance")
+    assert worst <= 1
