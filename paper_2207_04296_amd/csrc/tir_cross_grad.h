@@ -252,13 +252,17 @@ __global__ void __launch_bounds__(kGradThreads, 2) grad_rows_kernel(const GradPa
         const char* const q = (const char*)p.Q + 2 * (b * p.q_bs + m * p.q_rs + hq * p.q_hs) + g * 16;
         const char* const go = (const char*)p.dO + 2 * (b * p.g_bs + m * p.g_rs + hq * p.g_hs) + g * 16;
         const char* const o = (const char*)p.O + 2 * (b * p.o_bs + m * p.o_rs + hq * p.o_hs) + g * 16;
+        auto load = [&](auto with_o) __attribute__((always_inline)) {      // (a branch around each load of O would keep them behind each other)
 #pragma unroll
-        for (int ks = 0; ks < KSTEPS; ++ks) {
-            qf[ks] = *(const uint4*)(q + ks * 32);
-            of[ks] = *(const uint4*)(go + ks * 32);
-            if (!few) delta += dot8<DT>(of[ks], *(const uint4*)(o + ks * 32));
-        }
-        lse2 = p.lse[stat] * 1.44269504088896340736f;
+            for (int ks = 0; ks < KSTEPS; ++ks) {
+                qf[ks] = *(const uint4*)(q + ks * 32);
+                of[ks] = *(const uint4*)(go + ks * 32);
+                if constexpr (decltype(with_o)::value) delta += dot8<DT>(of[ks], *(const uint4*)(o + ks * 32));
+            }
+            lse2 = p.lse[stat] * 1.44269504088896340736f;
+        };
+        if (few) load(std::false_type());
+        else load(std::true_type());
     }
     const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (few && chunks > 0) {
