@@ -241,7 +241,7 @@ __global__ void __launch_bounds__(kGradThreads, 2) grad_rows_kernel(const GradPa
     const int m = (int)fastdiv((unsigned)row, p.div_g_magic, p.div_g_shift), hq = h * p.G + row - m * p.G;
     // D = dO . O, but of a sequence of one chunk sum_j P dP, whose terms are all at hand: O was rounded, and where few keys share a row's weight that error is as large as what dP - D leaves
     // (5 keys, bf16: dQ and dK
-    // off by 2.77e-3 relative in the mean, and this way by 2.36e-3, which is the rounding of dS and of the result).  O is not read then: 3 x 2500 x 19 keys x 56 query heads of 128 172 -> 152 us.
+    // off by 2.77e-3 relative in the mean, and this way by 2.36e-3, which is the rounding of dS and of the result).  O is not read then: 3 x 2500 x 19 keys x 56 query heads of 128 172 -> 144 us.
     const bool few = n <= kGradChunk;
     uint4 qf[KSTEPS], of[KSTEPS];
     float delta = 0.f, lse2 = 0.f;
