@@ -474,15 +474,34 @@ def tir_cross_attention(Q, K, V, O, lse, lens, batch, M, N, Hq, Hkv, d, q_bs, q_
         _check(st)
 
 
+def _gradient_strides(dO, shape, o_strides, g_strides, scale, in_dtype, stream):
+    """(g_bs, g_rs, g_hs, scale, in_dtype, stream) of a call that may have left out the strides of dO: scale, in_dtype and stream stand in their places then, unless they are named."""
+    given = [x for x in g_strides if x is not None]
+    if in_dtype is not None and scale is not None and len(given) == 3:
+        return (*given, scale, in_dtype, stream)
+    if in_dtype is None and scale is None and len(given) >= 2 and given == list(g_strides[:len(given)]):
+        scale, in_dtype, stream = *given[:2], given[2] if len(given) == 3 else stream
+    elif given or in_dtype is None or scale is None:
+        raise TypeError("tir_cross_attention_backward: all of g_bs, g_rs and g_hs or none of them, then scale and in_dtype")
+    if not hasattr(dO, "stride"):
+        return (*o_strides, scale, in_dtype, stream)
+    if tuple(dO.shape) != shape:
+        raise ValueError(f"tir_cross_attention_backward: g_bs, g_rs and g_hs can be left out for a dO of {shape}, got {tuple(dO.shape)}")
+    return (*dO.stride()[:3], scale, in_dtype, stream)
+
+
 def tir_cross_attention_backward_status(Q, K, V, O, dO, lse, lens, dQ, dK, dV, delta, batch, M, N, Hq, Hkv, d, q_bs, q_rs, q_hs, k_bs, k_rs, k_hs, v_bs, v_rs, v_hs,
-                                        o_bs, o_rs, o_hs, g_bs, g_rs, g_hs, scale, in_dtype, stream=0) -> int:
+                                        o_bs, o_rs, o_hs, g_bs=None, g_rs=None, g_hs=None, scale=None, in_dtype=None, stream=0) -> int:
+    g_bs, g_rs, g_hs, scale, in_dtype, stream = _gradient_strides(dO, (batch, M, Hq, d), (o_bs, o_rs, o_hs), (g_bs, g_rs, g_hs), scale, in_dtype, stream)
     return lib().tir_cross_attention_backward(*[_ptr(t) for t in (Q, K, V, O, dO, lse, lens, dQ, dK, dV, delta)], batch, M, N, Hq, Hkv, d, q_bs, q_rs, q_hs, k_bs, k_rs, k_hs,
                                               v_bs, v_rs, v_hs, o_bs, o_rs, o_hs, g_bs, g_rs, g_hs, float(scale), _code(in_dtype), stream)
 
 
 def tir_cross_attention_backward(Q, K, V, O, dO, lse, lens, dQ, dK, dV, delta, batch, M, N, Hq, Hkv, d, q_bs, q_rs, q_hs, k_bs, k_rs, k_hs, v_bs, v_rs, v_hs,
-                                 o_bs, o_rs, o_hs, g_bs, g_rs, g_hs, scale, in_dtype, stream=None) -> None:
-    """Gradients of tir_cross_attention; dQ, dK, dV with the strides of Q, K, V, dO with its own (g_*); delta: fp32 scratch [batch, Hq, M]."""
+                                 o_bs, o_rs, o_hs, g_bs=None, g_rs=None, g_hs=None, scale=None, in_dtype=None, stream=None) -> None:
+    """Gradients of tir_cross_attention; dQ, dK, dV with the strides of Q, K, V, dO with its own: g_bs, g_rs, g_hs, or none of the three and scale, in_dtype (and stream) right behind o_hs, for the
+    strides of a tensor dO [batch, M, Hq, d] as they are (of an address: those of O); delta: fp32 scratch [batch, Hq, M]."""
+    g_bs, g_rs, g_hs, scale, in_dtype, stream = _gradient_strides(dO, (batch, M, Hq, d), (o_bs, o_rs, o_hs), (g_bs, g_rs, g_hs), scale, in_dtype, stream)
     st = (_native or _load_native()).tir_cross_attention_backward(Q, K, V, O, dO, lse, lens, dQ, dK, dV, delta, batch, M, N, Hq, Hkv, d, q_bs, q_rs, q_hs, k_bs, k_rs, k_hs,
                                                                   v_bs, v_rs, v_hs, o_bs, o_rs, o_hs, g_bs, g_rs, g_hs, scale, in_dtype, stream)
     if st:
