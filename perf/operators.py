@@ -384,7 +384,7 @@ def run(s):
         return {"o": s["o"], "lse": s["lse"]} if case["lse"] else {"o": s["o"]}
     dk, dv = s["dkv"][:, :, 0], s["dkv"][:, :, 1]
     B.tir_cross_attention_backward(s["q"], s["k"], s["v"], s["o"], s["do"], s["lse"], s["lens"], s["dq"], dk, dv, s["delta"], batch, case["m"], case["n"], hq, heads, d,
-                                   *_strides(s["q"]), *_strides(s["k"]), *_strides(s["v"]), *_strides(s["o"]), *_strides(s["do"]), d ** -0.5, dt)
+                                   *_strides(s["q"]), *_strides(s["k"]), *_strides(s["v"]), *_strides(s["o"]), d ** -0.5, dt)
     return {"dq": s["dq"], "dk": dk, "dv": dv}
 
 
