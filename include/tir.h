@@ -266,13 +266,16 @@ tir_status tir_cross_attention(const void* Q, const void* K, const void* V, void
 
 /*
  * Gradients of tir_cross_attention: Q, K, V, lens, extents, strides and scale as in the forward call, O and lse its results (O in the input type), dO the gradient that
- * arrives, with strides g_bs, g_rs and g_hs of its own.  With P_ij = exp(scale * Q_i . K_j - lse_i) over j < lens[b], D_i = dO_i . O_i:
+ * arrives, with strides g_bs, g_rs and g_hs of its own.  With P_ij = exp(scale * Q_i . K_j - lse_i) over j < lens[b], D_i = sum_j P_ij (dO_i . V_j), which is dO_i . O_i:
  *     dV_j = sum_i P_ij dO_i     dS_ij = P_ij (dO_i . V_j - D_i)     dQ_i = scale * sum_j dS_ij K_j     dK_j = scale * sum_i dS_ij Q_i
  * the sums of dK and dV running over all query heads that share the key head as well.  dQ has Q's type and strides, dK and dV those of K and V; they are fully overwritten: rows of dK and
  * dV from lens[b] on are zeros, as are the rows of dQ of a sequence without keys.  A stride of Q, K or V that is 0 along an axis of more than one is refused: the gradients would overlap
- * (the gradient of a broadcast input is the sum over what it was broadcast to); other strides have to keep their rows apart, those of O and dO may be 0.  delta: scratch of the caller's, fp32 [batch][Hq][M]; holds D afterwards
- * (of sequences of up to 64 keys summed from P and dO . V, which O's rounding does not reach).
+ * (the gradient of a broadcast input is the sum over what it was broadcast to); other strides have to keep their rows apart, those of O and dO may be 0.  delta: scratch of the caller's, fp32 [batch][Hq][M]; holds D afterwards.
  * Nothing is added atomically: the same call gives the same bits.  P and dS are rounded to the input type for the last products (F16: times a power of two that uses the type's range), sums are fp32.
+ * D is summed from P and dO . V in fp32: dO . O, whose O was rounded, is its first estimate only, so that values far from zero cost no accuracy.  With u = 2^-11 (F16) or 2^-8 (BF16), a_ij = sum_c |dO_ic V_jc|,
+ * A_i = sum_j P_ij a_ij and s_ij = 2e-5 * P_ij * (a_ij + A_i), for scores of up to a hundred, besides u of the result and F16's subnormals:
+ *     |dV - exact| <= 1.05 u * sum_i P_ij |dO_i|                                  |delta - D| <= 2e-5 * A_i
+ *     |dQ - exact| <= |scale| * sum_j (1.05 u |dS_ij| + 4u^2 P_ij A_i + s_ij) |K_j|      |dK - exact| <= |scale| * sum_i (1.05 u |dS_ij| + s_ij) |Q_i|
  * With a workspace registered for `stream` few rows, or few keys, are shared among workgroups.
  * Conventions of pointers and strides as in the forward call; no tensor may overlap an output.  batch or Hq = 0 is a no-op.
  */

@@ -1,11 +1,16 @@
 // Gradients of the attention over another sequence's states.
 //
-// With P = exp(scale * Q K^T - lse), D_i = sum_c dO_ic O_ic (which is sum_j P_ij dP_ij) and dP = dO V^T:
+// With P = exp(scale * Q K^T - lse), dP = dO V^T and D_i = sum_j P_ij dP_ij (which is sum_c dO_ic O_ic):
 //     dS = P o (dP - D)     dV = P^T dO     dK = scale * dS^T Q     dQ = scale * dS K
 // Nothing of size M x N meets memory.  Two passes, each of which owns what it sums, so that nothing is added atomically and a result does not depend on
-// timing: one over rows (a workgroup keeps its queries and walks the keys: dQ), one over keys (keeps its keys and walks the queries: dK, dV).
-// S and dP are computed in both: 7 products instead of 5.  Both compute the transposes of S and dP resp. S and dP themselves such that a lane owns one row
+// timing: one over rows (a workgroup keeps its queries and walks the keys: dQ, D), one over keys (keeps its keys and walks the queries: dK, dV).
+// S and dP are computed in both: 8 products instead of 5.  Both compute the transposes of S and dP resp. S and dP themselves such that a lane owns one row
 // (one key), as in the forward pass: probabilities and dS come out of the first products in the layout in which the last ones read them.
+//
+// D.  O was rounded to 16 bits, and dO . O is off by that times |O|, however little dP - D is beside it (values of 8 and a tenth around it, bf16: dQ off by 0.16 of itself).  The pass over rows
+// therefore takes D' = dO . O for a first estimate only.  Over its walk it sums e = sum_j P (dP - D') = D - D', and P K beside dS' K, whose operands are the same:
+//     D = D' + e     dQ = scale * (sum_j dS'_ij K_j - e * sum_j P_ij K_j)
+// and the pass over keys reads that D.  What the roundings of P and dS' leave of the estimate's error is u^2 |dO| |O|, beside dS' own u |dS| (u: the input type's half step).
 //
 // LDS tiles [rows][128 bytes] per 64 channels are read both along their rows (S, dP) and across them (dQ, dK, dV: the transposing read).
 // 16-byte column c of row r is kept at column c ^ (4 * (r/2 mod 2) + r/4 mod 4): the 16 rows of a ds_read_b128 phase meet all banks once, and the 8 rows
@@ -22,7 +27,7 @@ struct GradParams {
     const void *Q, *K, *V, *O, *dO;
     void *dQ, *dK, *dV;
     const float* lse;        // [batch][query heads][M]
-    float* delta;            // the same: D, written by the pass over rows
+    float* delta;            // the same: D, written by the pass over rows (its slices' sum)
     const int* lens;         // null: N each
     long long q_bs, q_rs, q_hs, k_bs, k_rs, k_hs, v_bs, v_rs, v_hs, o_bs, o_rs, o_hs, g_bs, g_rs, g_hs;      // (g: dO)
     int q_near;              // 128 positions and all heads of a group lie within 2^31 bytes of dQ
@@ -36,7 +41,10 @@ struct GradParams {
 };
 
 constexpr int kGradWaves = 4, kGradThreads = 64 * kGradWaves, kGradTile = 32 * kGradWaves;      // rows resp. keys of a workgroup
-constexpr int kGradChunk = 64;      // keys resp. rows of a step
+constexpr int kFewKeys = 64;        // up to so many keys are one chunk of the pass over rows
+
+// Partial sums of a slice, in floats.  Rows: dS' K, P K and the rows' e; keys: dK and dV.
+constexpr int grad_partial(bool keys, int d) { return 2 * kGradTile * d + (keys ? 0 : kGradTile); }
 
 hipError_t launch_grad_rows(const GradParams& p, int dt, int dh, hipStream_t stream);
 hipError_t launch_grad_keys(const GradParams& p, int dt, int dh, hipStream_t stream);
@@ -64,9 +72,10 @@ template <int DH, int RB> struct GradTile {
         }
     }
     // Operand of k-step ks (16 channels): row l31 of the 32 from row r0
-    static __device__ __forceinline__ uint4 along(const char* tile, int r0, int ks, int l31, int g) {
-        return *(const uint4*)(tile + (ks >> 2) * HALF + (r0 + l31) * 128 + ((((ks & 3) * 2 + g) ^ grad_swz(l31)) << 4));
+    static __device__ __forceinline__ const char* along_at(const char* tile, int r0, int ks, int l31, int g) {
+        return tile + (ks >> 2) * HALF + (r0 + l31) * 128 + ((((ks & 3) * 2 + g) ^ grad_swz(l31)) << 4);
     }
+    static __device__ __forceinline__ uint4 along(const char* tile, int r0, int ks, int l31, int g) { return *(const uint4*)along_at(tile, r0, ks, l31, g); }
     // Operand of the 16 rows from r0 for channels 32*db ..: position (g, 4*hh + e) is row r0 + 8*hh + 4*g + e, the order of a product's result registers
     static __device__ __forceinline__ uint4 across(const char* tile, int r0, int db, int blk, int s16) {
         i16x4 h[2];
@@ -198,14 +207,24 @@ template <int N, int LA, class READ, class MUL> __device__ __forceinline__ void 
 }
 
 // ---------------------------------------------------------------------------------------------
-// dQ: four waves of 32 rows (position, query head) each; keys and values through two LDS stages.
+// dQ and D: four waves of 32 rows (position, query head) each; keys and values through two LDS stages.
+//
+// FEW: calls of up to kFewKeys keys.  All terms of D are at hand before the first dS is formed, so it is summed from them and neither O nor P K is needed
+// (3 x 2500 x 19 keys x 56 query heads of 128: 172 us when O was read, 144 without).
+// Otherwise, at d = 128, the two sums are 128 registers and the queries 32; dO is kept in LDS, beside chunks of half as many keys.  The second sum costs a third of the matrix work and half of
+// the vector registers: both passes with and without it, 2 x 2047 x 4095 and 1365 keys x 16 / 4 heads of 128 400 and 353 us, 16 x 250 x 333 x 12 heads of 64 33.4 and 31.9 (two workgroups per CU and three).
 // ---------------------------------------------------------------------------------------------
-template <int DT, int DH>
+template <int DT, int DH, bool FEW>
 __global__ void __launch_bounds__(kGradThreads, 2) grad_rows_kernel(const GradParams p) {
-    typedef GradTile<DH, kGradChunk> T;
-    constexpr int KSTEPS = DH / 16, DB = DH / 32, STAGE = 2 * T::BYTES;
-    static_assert(2 * STAGE >= kGradTile * DH * 2, "the output tile is staged in the rings");
-    __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
+    constexpr int CH = FEW || DH == 64 ? 64 : 32;      // keys of a chunk
+    constexpr bool G_LDS = !FEW && DH == 128;
+    constexpr int LA = 2;
+    static_assert(!FEW || CH == kFewKeys, "");
+    typedef GradTile<DH, CH> T;
+    typedef GradTile<DH, kGradTile> GT;
+    constexpr int KSTEPS = DH / 16, DB = DH / 32, STAGE = 2 * T::BYTES, RING = (FEW ? 1 : 2) * STAGE;
+    static_assert(RING >= kGradTile * DH * 2, "the output tile is staged in the ring");
+    __shared__ __attribute__((aligned(1024))) char smem[RING + (G_LDS ? GT::BYTES : 0)];
     const int lane = threadIdx.x & 63, l31 = lane & 31, g = lane >> 5, blk = lane >> 4, s16 = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int bh = (int)fastdiv(blockIdx.x, p.div_tiles_magic, p.div_tiles_shift);
@@ -217,9 +236,9 @@ __global__ void __launch_bounds__(kGradThreads, 2) grad_rows_kernel(const GradPa
         n = p.lens[b];
         n = n < 0 ? 0 : (n > p.N ? p.N : n);
     }
-    const int chunks_all = (n + kGradChunk - 1) / kGradChunk;
-    const int per = (chunks_all + p.slices - 1) / p.slices;
-    const int c0 = (int)blockIdx.y * per;
+    const int chunks_all = (n + CH - 1) / CH;
+    const int per = FEW ? chunks_all : (chunks_all + p.slices - 1) / p.slices;
+    const int c0 = FEW ? 0 : (int)blockIdx.y * per;
     const int chunks = chunks_all - c0 < per ? chunks_all - c0 : per;      // may be none: this slice's sums are zeros
 
     const char* const Kb = (const char*)p.K + 2 * (b * p.k_bs + h * p.k_hs);
@@ -227,8 +246,8 @@ __global__ void __launch_bounds__(kGradThreads, 2) grad_rows_kernel(const GradPa
     const int k_rs = (int)p.k_rs, v_rs = (int)p.v_rs;
     const unsigned k_off = T::lane_offset(wave, lane, k_rs), v_off = T::lane_offset(wave, lane, v_rs);
     auto copy = [&](int i) __attribute__((always_inline)) {
-        char* const st = smem + (i & 1) * STAGE;
-        const long long key = (long long)(c0 + i) * kGradChunk;
+        char* const st = smem + (FEW ? 0 : (i & 1) * STAGE);
+        const long long key = (long long)(c0 + i) * CH;
         const int left = i < chunks ? n - (int)key : 0;
         T::copy(st, Kb + key * k_rs * 2, left, k_rs, k_off, wave, lane);
         T::copy(st + T::BYTES, Vb + key * v_rs * 2, left, v_rs, v_off, wave, lane);
@@ -239,33 +258,45 @@ __global__ void __launch_bounds__(kGradThreads, 2) grad_rows_kernel(const GradPa
     const int row = row0 + wave * 32 + l31;
     const bool live = wave * 32 + l31 < rows;
     const int m = (int)fastdiv((unsigned)row, p.div_g_magic, p.div_g_shift), hq = h * p.G + row - m * p.G;
-    // D = dO . O, but of a sequence of one chunk sum_j P dP, whose terms are all at hand: O was rounded, and where few keys share a row's weight that error is as large as what dP - D leaves
-    // (5 keys, bf16: dQ and dK
-    // off by 2.77e-3 relative in the mean, and this way by 2.36e-3, which is the rounding of dS and of the result).  O is not read then: 3 x 2500 x 19 keys x 56 query heads of 128 172 -> 144 us.
-    const bool few = n <= kGradChunk;
-    uint4 qf[KSTEPS], of[KSTEPS];
+    uint4 qf[KSTEPS], of[G_LDS ? 1 : KSTEPS];
     float delta = 0.f, lse2 = 0.f;
     const long long stat = ((long long)b * p.heads * p.G + hq) * p.M + m;
+    char* const g_tile = smem + RING;                  // G_LDS: a wave writes and reads its own 32 rows
 #pragma unroll
-    for (int ks = 0; ks < KSTEPS; ++ks) qf[ks] = of[ks] = make_uint4(0, 0, 0, 0);
-    if (live) {
+    for (int ks = 0; ks < KSTEPS; ++ks) qf[ks] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int ks = 0; ks < (G_LDS ? 1 : KSTEPS); ++ks) of[ks] = make_uint4(0, 0, 0, 0);
+    {
         const char* const q = (const char*)p.Q + 2 * (b * p.q_bs + m * p.q_rs + hq * p.q_hs) + g * 16;
         const char* const go = (const char*)p.dO + 2 * (b * p.g_bs + m * p.g_rs + hq * p.g_hs) + g * 16;
         const char* const o = (const char*)p.O + 2 * (b * p.o_bs + m * p.o_rs + hq * p.o_hs) + g * 16;
-        auto load = [&](auto with_o) __attribute__((always_inline)) {      // (a branch around each load of O would keep them behind each other)
+        if constexpr (G_LDS) {
+            uint4 x[KSTEPS];
+#pragma unroll
+            for (int ks = 0; ks < KSTEPS; ++ks) x[ks] = make_uint4(0, 0, 0, 0);
+            if (live) {
+#pragma unroll
+                for (int ks = 0; ks < KSTEPS; ++ks) {
+                    x[ks] = *(const uint4*)(go + ks * 32);
+                    delta += dot8<DT>(x[ks], *(const uint4*)(o + ks * 32));
+                }
+            }
+#pragma unroll
+            for (int ks = 0; ks < KSTEPS; ++ks) *(uint4*)(g_tile + (GT::along_at(g_tile, wave * 32, ks, l31, g) - g_tile)) = x[ks];
+            TIR_FENCE();
+        }
+        if (live) {
 #pragma unroll
             for (int ks = 0; ks < KSTEPS; ++ks) {
                 qf[ks] = *(const uint4*)(q + ks * 32);
-                of[ks] = *(const uint4*)(go + ks * 32);
-                if constexpr (decltype(with_o)::value) delta += dot8<DT>(of[ks], *(const uint4*)(o + ks * 32));
+                if constexpr (!G_LDS) of[ks] = *(const uint4*)(go + ks * 32);
+                if constexpr (!G_LDS && !FEW) delta += dot8<DT>(of[ks], *(const uint4*)(o + ks * 32));
             }
             lse2 = p.lse[stat] * 1.44269504088896340736f;
-        };
-        if (few) load(std::false_type());
-        else load(std::true_type());
+        }
     }
     const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (few && chunks > 0) {
+    if (FEW && chunks > 0) {
         copy_barrier<0>();
 #pragma unroll 1
         for (int jb = 0; jb * 32 < n; ++jb) {
@@ -279,66 +310,119 @@ __global__ void __launch_bounds__(kGradThreads, 2) grad_rows_kernel(const GradPa
         }
     }
     delta += __shfl_xor(delta, 32);
-    if (live && g == 0 && blockIdx.y == 0) p.delta[stat] = delta;
 
-    f32x16 acc[DB];
+    f32x16 acc[DB], pk[FEW ? 1 : DB];                  // sums of dS' K and of P K
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) acc[db][r] = 0.f;
-    float by = DT == DT_F16 ? kFirstFactor : 1.f;
+        for (int r = 0; r < 16; ++r) acc[db][r] = pk[FEW ? 0 : db][r] = 0.f;
+    float by = DT == DT_F16 ? kFirstFactor : 1.f, e_sum = 0.f;
+    const float ref2 = FEW ? -lse2 : p_factor_log2<DT>() - lse2, pf = FEW || DT != DT_F16 ? 1.f : 0x1p-14f;      // (a probability that is an operand is held times 2^14 in F16)
 
     for (int i = 0; i < chunks; ++i) {
         copy_barrier<0>();                     // chunk i is in, and everybody is past chunk i - 1
         if (i + 1 < chunks) copy(i + 1);
-        const char* const tk = smem + (i & 1) * STAGE;
+        const char* const tk = smem + (FEW ? 0 : (i & 1) * STAGE);
         const char* const tv = tk + T::BYTES;
 #pragma unroll
-        for (int jb = 0; jb < kGradChunk / 32; ++jb) {
-            const int left = n - (c0 + i) * kGradChunk - jb * 32;      // keys of this block
+        for (int jb = 0; jb < CH / 32; ++jb) {
+            const int left = n - (c0 + i) * CH - jb * 32;      // keys of this block
             if (left <= 0) break;
             f32x16 s, dp;
+            unsigned w[8], pw[8];
+            if constexpr (FEW) {
 #pragma unroll
-            for (int ks = 0; ks < KSTEPS; ++ks) s = InTraits<DT>::mfma(T::along(tk, jb * 32, ks, l31, g), qf[ks], ks == 0 ? zero16 : s);
+                for (int ks = 0; ks < KSTEPS; ++ks) s = InTraits<DT>::mfma(T::along(tk, jb * 32, ks, l31, g), qf[ks], ks == 0 ? zero16 : s);
 #pragma unroll
-            for (int ks = 0; ks < KSTEPS; ++ks) dp = InTraits<DT>::mfma(T::along(tv, jb * 32, ks, l31, g), of[ks], ks == 0 ? zero16 : dp);
-            f32x16 ds;
+                for (int ks = 0; ks < KSTEPS; ++ks) dp = InTraits<DT>::mfma(T::along(tv, jb * 32, ks, l31, g), of[ks], ks == 0 ? zero16 : dp);
+            } else {
+                products<KSTEPS, LA>([&](int ks) __attribute__((always_inline)) { return T::along(tk, jb * 32, ks, l31, g); },
+                                     [&](int ks, const uint4& x) __attribute__((always_inline)) { s = InTraits<DT>::mfma(x, qf[ks], ks == 0 ? zero16 : s); });
+            }
 #pragma unroll
-            for (int r = 0; r < 16; ++r) ds[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], p.scale_log2e, -lse2)) * (dp[r] - delta);
+            for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], p.scale_log2e, ref2));
             if (left < 32) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) ds[r] = 8 * (r >> 2) + 4 * g + (r & 3) < left ? ds[r] : 0.f;
+                for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + 4 * g + (r & 3) < left ? s[r] : 0.f;
             }
-            unsigned w[8];
-            round_ds<DT, DB>(ds, by, acc, w);
+            if constexpr (G_LDS)
+                products<KSTEPS, LA>([&](int ks) __attribute__((always_inline)) { return TwoOperands{T::along(tv, jb * 32, ks, l31, g), GT::along(g_tile, wave * 32, ks, l31, g)}; },
+                                     [&](int ks, const TwoOperands& x) __attribute__((always_inline)) { dp = InTraits<DT>::mfma(x.a, x.b, ks == 0 ? zero16 : dp); });
+            else if constexpr (!FEW)
+                products<KSTEPS, LA>([&](int ks) __attribute__((always_inline)) { return T::along(tv, jb * 32, ks, l31, g); },
+                                     [&](int ks, const uint4& x) __attribute__((always_inline)) { dp = InTraits<DT>::mfma(x, of[ks], ks == 0 ? zero16 : dp); });
+            f32x16 ds;
 #pragma unroll
-            for (int ss = 0; ss < 2; ++ss) {
-                const uint4 df = make_uint4(w[4 * ss], w[4 * ss + 1], w[4 * ss + 2], w[4 * ss + 3]);
+            for (int r = 0; r < 16; ++r) ds[r] = s[r] * (dp[r] - delta);
+            if constexpr (FEW) {
+                round_ds<DT, DB>(ds, by, acc, w);
 #pragma unroll
-                for (int db = 0; db < DB; ++db) acc[db] = InTraits<DT>::mfma(T::across(tk, jb * 32 + ss * 16, db, blk, s16), df, acc[db]);
+                for (int ss = 0; ss < 2; ++ss) {
+                    const uint4 df = make_uint4(w[4 * ss], w[4 * ss + 1], w[4 * ss + 2], w[4 * ss + 3]);
+#pragma unroll
+                    for (int db = 0; db < DB; ++db) acc[db] = InTraits<DT>::mfma(T::across(tk, jb * 32 + ss * 16, db, blk, s16), df, acc[db]);
+                }
+            } else {
+#pragma unroll
+                for (int r = 0; r < 8; ++r) pw[r] = grad_pack<DT>(s[2 * r], s[2 * r + 1]);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) e_sum += ds[r];
+                round_ds<DT, DB>(ds, by, acc, w);
+                products<2 * DB, LA>([&](int t) __attribute__((always_inline)) { return T::across(tk, jb * 32 + t / DB * 16, t % DB, blk, s16); },
+                                     [&](int t, const uint4& x) __attribute__((always_inline)) {
+                                         const int at = t / DB * 4;
+                                         acc[t % DB] = InTraits<DT>::mfma(x, make_uint4(w[at], w[at + 1], w[at + 2], w[at + 3]), acc[t % DB]);
+                                         pk[t % DB] = InTraits<DT>::mfma(x, make_uint4(pw[at], pw[at + 1], pw[at + 2], pw[at + 3]), pk[t % DB]);
+                                     });
+#pragma unroll
+                for (int db = 0; db < DB; ++db) {
+                    here(acc[db]);
+                    here(pk[db]);
+                }
             }
             TIR_FENCE();                       // (the next block's operands read ahead of here would not fit the registers)
         }
     }
-    const float f = p.scale / by;
-    if (p.slices > 1) {
-        if (wave * 32 >= rows) return;                   // (nobody reads these)
-        // [tile][slice][wave][db][quarter][lane] of four values
-        typedef float f32x4 __attribute__((ext_vector_type(4)));
-        f32x4* const o = (f32x4*)p.ws + ((long long)blockIdx.x * p.slices + blockIdx.y) * (kGradTile * DH / 4) + wave * (32 * DH / 4) + lane;
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-            for (int q4 = 0; q4 < 4; ++q4) o[(db * 4 + q4) * 64] = f32x4{acc[db][4 * q4] * f, acc[db][4 * q4 + 1] * f, acc[db][4 * q4 + 2] * f, acc[db][4 * q4 + 3] * f};
-        return;
+    const float f = p.scale * pf / by;
+    e_sum = (e_sum + __shfl_xor(e_sum, 32)) * pf;
+    const bool whole = FEW || p.slices == 1;
+    if (live && g == 0 && (whole || blockIdx.y == 0)) {
+        // (the row's place once more: held over the loop, its registers would be short there)
+        int r = row0 + wave * 32 + l31;
+        asm volatile("" : "+v"(r));
+        const int mr = (int)fastdiv((unsigned)r, p.div_g_magic, p.div_g_shift);
+        p.delta[((long long)b * p.heads * p.G + h * p.G + r - mr * p.G) * p.M + mr] = whole ? delta + e_sum : delta;
     }
-    __syncthreads();                           // the rings are free
+    const float fp = -(p.scale * pf) * e_sum;
+    if constexpr (!FEW) {
+        if (p.slices > 1) {
+            if (wave * 32 >= rows) return;               // (nobody reads these)
+            // [tile][slice]: dS' K and P K, [wave][db][quarter][lane] of four values each, and e of the rows
+            typedef float f32x4 __attribute__((ext_vector_type(4)));
+            float* const part = p.ws + ((long long)blockIdx.x * p.slices + blockIdx.y) * grad_partial(false, DH);
+            f32x4* const o = (f32x4*)part + wave * (32 * DH / 4) + lane;
+            const float fk = p.scale * pf;
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int q4 = 0; q4 < 4; ++q4) {
+                    o[(db * 4 + q4) * 64] = f32x4{acc[db][4 * q4] * f, acc[db][4 * q4 + 1] * f, acc[db][4 * q4 + 2] * f, acc[db][4 * q4 + 3] * f};
+                    o[(db * 4 + q4) * 64 + kGradTile * DH / 4] = f32x4{pk[db][4 * q4] * fk, pk[db][4 * q4 + 1] * fk, pk[db][4 * q4 + 2] * fk, pk[db][4 * q4 + 3] * fk};
+                }
+            if (g == 0) part[2 * kGradTile * DH + wave * 32 + l31] = e_sum;
+            return;
+        }
+    }
+    __syncthreads();                           // the ring is free
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4)
-            grad_stage<DH>(smem, wave * 32 + l31, db * 32 + q4 * 8 + 4 * g,
-                           make_uint2(grad_pack<DT>(acc[db][4 * q4] * f, acc[db][4 * q4 + 1] * f), grad_pack<DT>(acc[db][4 * q4 + 2] * f, acc[db][4 * q4 + 3] * f)));
+        for (int q4 = 0; q4 < 4; ++q4) {
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = FEW ? acc[db][4 * q4 + e] * f : __builtin_fmaf(pk[FEW ? 0 : db][4 * q4 + e], fp, acc[db][4 * q4 + e] * f);
+            grad_stage<DH>(smem, wave * 32 + l31, db * 32 + q4 * 8 + 4 * g, make_uint2(grad_pack<DT>(v[0], v[1]), grad_pack<DT>(v[2], v[3])));
+        }
     __syncthreads();
     const int first_m = (int)fastdiv((unsigned)row0, p.div_g_magic, p.div_g_shift);
     unsigned short* const base = (unsigned short*)p.dQ + b * p.q_bs + (long long)h * p.G * p.q_hs + first_m * p.q_rs;
@@ -537,7 +621,7 @@ __global__ void __launch_bounds__(kGradThreads * RG, DH == 64 && RG == 1 ? 3 : 2
     static_assert(RG > 1 || kGradWaves * 32 * DH * 2 <= LDS, "");
     if (p.slices > 1) {
         if (key0 + wave * 32 >= p.N) return;             // (nobody reads these)
-        f32x4* const o = (f32x4*)p.ws + ((long long)blockIdx.x * p.slices + blockIdx.y) * (2 * kGradTile * DH / 4) + wave * (32 * DH / 4) + lane;
+        f32x4* const o = (f32x4*)(p.ws + ((long long)blockIdx.x * p.slices + blockIdx.y) * grad_partial(true, DH)) + wave * (32 * DH / 4) + lane;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -567,36 +651,47 @@ __global__ void __launch_bounds__(kGradThreads * RG, DH == 64 && RG == 1 ? 3 : 2
 }
 
 // ---------------------------------------------------------------------------------------------
-// The slices' partial sums, added in slice order: one thread per four values of a tile.  KEYS: dK (the first half of a partial) and dV.
+// The slices' partial sums, added in slice order: one thread per four values of a tile.  KEYS: dK (the first half of a partial) and dV.  Rows: dQ = sum of dS' K - e * sum of P K, and D.
 // ---------------------------------------------------------------------------------------------
 template <int DT, int DH, bool KEYS> __global__ void __launch_bounds__(256) grad_sum_kernel(const GradParams p) {
     typedef float f32x4 __attribute__((ext_vector_type(4)));
-    constexpr int PART = (KEYS ? 2 : 1) * kGradTile * DH / 4;
-    const int tile = (int)blockIdx.y, at = (int)(blockIdx.x * 256 + threadIdx.x);      // < PART: a multiple of 256
+    constexpr int PART = grad_partial(KEYS, DH) / 4, HALF = kGradTile * DH / 4;
+    const int tile = (int)blockIdx.y, at = (int)(blockIdx.x * 256 + threadIdx.x);      // < (KEYS ? 2 : 1) * HALF: a multiple of 256
     const int bh = (int)fastdiv((unsigned)tile, p.div_tiles_magic, p.div_tiles_shift);
     const int b = (int)fastdiv((unsigned)bh, p.div_h_magic, p.div_h_shift), h = bh - b * p.heads;
-    const int in = at % (kGradTile * DH / 4), lane = in & 63, grp = in >> 6;       // grp = wave * (DH / 8) + db * 4 + quarter
-    const int row = (tile - bh * p.tiles) * kGradTile + grp / (DH / 8) * 32 + (lane & 31);
+    const int in = at % HALF, lane = in & 63, grp = in >> 6;       // grp = wave * (DH / 8) + db * 4 + quarter
+    const int in_tile = grp / (DH / 8) * 32 + (lane & 31), row = (tile - bh * p.tiles) * kGradTile + in_tile;
     const int ch = grp % (DH / 8) * 8 + 4 * (lane >> 5);
     if (row >= (KEYS ? p.N : p.M * p.G)) return;                                    // (what no pass writes)
     const f32x4* const part = (const f32x4*)p.ws + (long long)tile * p.slices * PART + at;
     f32x4 sum = part[0];
-#pragma unroll 4
-    for (int z = 1; z < p.slices; ++z) sum += part[(long long)z * PART];
-    const uint2 v = make_uint2(grad_pack<DT>(sum[0], sum[1]), grad_pack<DT>(sum[2], sum[3]));
     if constexpr (KEYS) {
-        int n = p.N;
-        if (p.lens) {
-            n = p.lens[b];
-            n = n < 0 ? 0 : (n > p.N ? p.N : n);
-        }
-        const bool second = at >= kGradTile * DH / 4;
-        unsigned short* const o = second ? (unsigned short*)p.dV + b * p.v_bs + row * p.v_rs + h * p.v_hs : (unsigned short*)p.dK + b * p.k_bs + row * p.k_rs + h * p.k_hs;
-        *(uint2*)(o + ch) = row < n ? v : make_uint2(0, 0);
+#pragma unroll 4
+        for (int z = 1; z < p.slices; ++z) sum += part[(long long)z * PART];
     } else {
+        f32x4 pk = part[HALF];
+        const float* const e_at = p.ws + (long long)tile * p.slices * (4 * PART) + 2 * kGradTile * DH + in_tile;
+        float e = e_at[0];
+#pragma unroll 4
+        for (int z = 1; z < p.slices; ++z) {
+            sum += part[(long long)z * PART];
+            pk += part[(long long)z * PART + HALF];
+            e += e_at[(long long)z * (4 * PART)];
+        }
+        sum -= e * pk;
         const int m = (int)fastdiv((unsigned)row, p.div_g_magic, p.div_g_shift), hq = h * p.G + row - m * p.G;
-        *(uint2*)((unsigned short*)p.dQ + b * p.q_bs + m * p.q_rs + hq * p.q_hs + ch) = v;
+        if (ch == 0) p.delta[((long long)b * p.heads * p.G + hq) * p.M + m] += e;
+        *(uint2*)((unsigned short*)p.dQ + b * p.q_bs + m * p.q_rs + hq * p.q_hs + ch) = make_uint2(grad_pack<DT>(sum[0], sum[1]), grad_pack<DT>(sum[2], sum[3]));
+        return;
     }
+    const uint2 v = make_uint2(grad_pack<DT>(sum[0], sum[1]), grad_pack<DT>(sum[2], sum[3]));
+    int n = p.N;
+    if (p.lens) {
+        n = p.lens[b];
+        n = n < 0 ? 0 : (n > p.N ? p.N : n);
+    }
+    unsigned short* const o = at >= HALF ? (unsigned short*)p.dV + b * p.v_bs + row * p.v_rs + h * p.v_hs : (unsigned short*)p.dK + b * p.k_bs + row * p.k_rs + h * p.k_hs;
+    *(uint2*)(o + ch) = row < n ? v : make_uint2(0, 0);
 }
 
 }  // namespace tir

@@ -11,7 +11,7 @@ template <int DT, int DH, bool KEYS> static hipError_t launch_pass(const GradPar
     const unsigned tiles = (unsigned)(p.batch * p.heads * p.tiles);
     const dim3 grid(tiles, (unsigned)p.slices);
     hipError_t e;
-    if (!KEYS) e = launch_kernel(&grad_rows_kernel<DT, DH>, grid, dim3(kGradThreads), stream, p);
+    if (!KEYS) e = launch_kernel(p.N <= kFewKeys ? &grad_rows_kernel<DT, DH, true> : &grad_rows_kernel<DT, DH, false>, grid, dim3(kGradThreads), stream, p);
     else if ((int64_t)tiles * p.slices <= 256) e = launch_kernel(&grad_keys_kernel<DT, DH, 2>, grid, dim3(2 * kGradThreads), stream, p);
     else e = launch_kernel(&grad_keys_kernel<DT, DH, 1>, grid, dim3(kGradThreads), stream, p);
     if (e != hipSuccess || p.slices == 1) return e;
@@ -27,7 +27,7 @@ template <bool KEYS> static hipError_t launch_by_type(const GradParams& p, int d
 hipError_t launch_grad_rows(const GradParams& p, int dt, int dh, hipStream_t stream) { return launch_by_type<false>(p, dt, dh, stream); }
 hipError_t launch_grad_keys(const GradParams& p, int dt, int dh, hipStream_t stream) { return launch_by_type<true>(p, dt, dh, stream); }
 
-// How many workgroups share a tile's walk of `steps` chunks: as many as the chip has room for, each with two chunks at least, as far as the partial sums fit.
+// How many workgroups share a tile's walk of `steps` chunks (of 64 rows or keys): as many as the chip has room for, each with two chunks at least, as far as the partial sums fit.
 static int slices_of(int64_t tiles, int64_t room, int64_t steps, int64_t part_bytes, const StreamWorkspace& ws) {
     if (!ws.partial || tiles >= room) return 1;
     int64_t s = room / tiles;
@@ -94,13 +94,13 @@ tir_status tir_cross_attention_backward(const void* Q, const void* K, const void
         const FastDiv dt = make_fastdiv((unsigned)tiles);
         p.tiles = (int)tiles;
         p.div_tiles_magic = dt.magic; p.div_tiles_shift = dt.shift;
-        p.slices = slices_of(batch * Hkv * tiles, keys ? 256 : 512, steps, kGradTile * d * 4 * (keys ? 2 : 1), ws);
+        p.slices = slices_of(batch * Hkv * tiles, keys ? 256 : 512, steps, 4 * grad_partial(keys, (int)d), ws);
         return keys ? launch_grad_keys(p, (int)in, (int)d, (hipStream_t)stream) : launch_grad_rows(p, (int)in, (int)d, (hipStream_t)stream);
     };
     const int64_t row_tiles = (M * p.G + kGradTile - 1) / kGradTile, key_tiles = (N + kGradTile - 1) / kGradTile;
     if (!grid_fits(batch * Hkv * row_tiles, kGradThreads) || !grid_fits(batch * Hkv * key_tiles, kGradThreads)) return launch_error(who, hipErrorInvalidConfiguration);
     hipError_t e = hipSuccess;
-    if (M > 0) e = pass(false, row_tiles, (N + kGradChunk - 1) / kGradChunk);
+    if (M > 0) e = pass(false, row_tiles, (N + 63) / 64);
     if (e == hipSuccess && N > 0) e = pass(true, key_tiles, (M + 63) / 64 * p.G);
     if (e != hipSuccess) return launch_error(who, e);
     return TIR_OK;

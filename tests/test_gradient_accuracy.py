@@ -1,0 +1,104 @@
+"""Gradients where D_i = sum_j P_ij dP_ij is large beside what dP - D leaves: values far from zero, peaked probabilities, keys with a mean.
+
+Tolerances, per element, with u the input type's half step, a_ij = sum_c |dO_ic| |V_jc| and its mean A_i = sum_j P_ij a_ij:
+  - the estimate of D from the forward pass's output is off by E_i <= 2u A_i (probabilities and output rounded once each), and taken back to fp32 sums: of d terms in dP, of n in D, each at most
+    128 * 2^-24 < 8e-6 of their magnitudes when they add up without cancelling, so D is within 2e-5 A_i and dP within 2e-5 a_ij;
+  - dQ: dS' = P (dP - D') is rounded once, u (|dS| + P E); the P that goes with the correction once, u P E; so u |dS| + 4u^2 P A + 2e-5 P (a + A), times |K|, times scale;
+  - dK: u |dS| + 2e-5 P (a + A), times |Q|, times scale;
+  - the result is rounded to u of itself, F16 subnormals to 2^-25.  (1.01 for u^2 and the exponentials' last bits.)"""
+import pytest
+
+from paper_2207_04296_amd import binding as B
+from tests import decoder_reference as R
+from tests.test_cross_attention_gradients import U, _forward_and_backward, workspace  # noqa: F401  (a fixture)
+
+HEADS, M = 2, 50
+# values: (mean, spread), size of the queries, mean of the keys
+DATA = [((8.0, 0.1), 1.0, 0.0), ((2.0, 1.0), 1.0, 0.0), ((0.0, 1.0), 4.0, 0.0), ((8.0, 0.1), 1.0, 3.0), ((-100.0, 1.0), 1.0, 0.0)]
+LENS = [[65], [77], [128], [129, 64, 5, 65], [333, 64, 128], [1500, 300]]
+
+
+def _inputs(dtype, d, lens, data):
+    import torch
+    (mean, spread), size, shift = data
+    g, t = torch.Generator().manual_seed(len(lens) + lens[0] + d), R.TORCH[dtype]
+    n = max(lens)
+    q = (torch.randn((len(lens), M, HEADS, d), generator=g) * size).to(t)
+    k = (torch.randn((len(lens), n, HEADS, d), generator=g) + shift).to(t)
+    v = (mean + spread * torch.randn((len(lens), n, HEADS, d), generator=g)).to(t)
+    return q, k, v, torch.randn(q.shape, generator=g).to(t)
+
+
+def _worst(dtype, lens, scale, q, k, v, do, got):
+    """The largest share of its tolerance that an element of dq, dk and delta takes."""
+    import torch
+    u = U[dtype]
+    worst = {"dq": 0.0, "dk": 0.0, "delta": 0.0}
+    for b, length in enumerate(lens):
+        Q, K, V, G = (x[b, :y].double().transpose(0, 1) for x, y in ((q, M), (k, length), (v, length), (do, M)))
+        P = torch.softmax(scale * Q @ K.transpose(1, 2), -1)
+        dP, a = G @ V.transpose(1, 2), G.abs() @ V.abs().transpose(1, 2)
+        D, A = (P * dP).sum(-1, keepdim=True), (P * a).sum(-1, keepdim=True)
+        dS = P * (dP - D)
+        sums = 1.01 * u * dS.abs() + 2e-5 * P * (a + A)
+        for name, ref, mag, out in (("dq", dS @ K, (sums + 4 * u * u * P * A) @ K.abs(), got["dq"][b]), ("dk", dS.transpose(1, 2) @ Q, sums.transpose(1, 2) @ Q.abs(), got["dk"][b, :length])):
+            ref, mag = scale * ref.transpose(0, 1), scale * mag.transpose(0, 1)
+            worst[name] = max(worst[name], float(((out.double() - ref).abs() / (mag + u * ref.abs() + 2.0 ** -25)).nan_to_num(nan=1e9).max()))
+        worst["delta"] = max(worst["delta"], float(((got["delta"][b].double() - D.squeeze(-1)).abs() / (2e-5 * A.squeeze(-1))).nan_to_num(nan=1e9).max()))
+    return worst
+
+
+def _emulated(dtype, lens, scale, q, k, v, do, corrected):
+    """The gradients' arithmetic in fp32 with its roundings; not corrected: D from the rounded output alone."""
+    import torch
+    t = R.TORCH[dtype]
+    r = lambda x: x.to(t).float()  # noqa: E731
+    out = {"dq": torch.zeros(q.shape), "dk": torch.zeros(k.shape), "delta": torch.zeros((len(lens), HEADS, M))}
+    for b, length in enumerate(lens):
+        Q, K, V, G = (x[b, :y].float().transpose(0, 1) for x, y in ((q, M), (k, length), (v, length), (do, M)))
+        P = torch.softmax(scale * Q @ K.transpose(1, 2), -1)
+        dP = G @ V.transpose(1, 2)
+        D = (G * r(P @ V)).sum(-1, keepdim=True)
+        dS = P * (dP - D)
+        dq = r(dS) @ K
+        if corrected:
+            e = dS.sum(-1, keepdim=True)
+            dq, D = dq - e * (r(P) @ K), D + e
+            dS = P * (dP - D)
+        out["dq"][b] = r(scale * dq).transpose(0, 1)
+        out["dk"][b, :length] = r(scale * r(dS).transpose(1, 2) @ Q).transpose(0, 1)
+        out["delta"][b] = D.squeeze(-1)
+    return out
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_the_tolerances_tell_a_rounded_output_from_a_corrected_one(dtype):
+    for lens in LENS[:4]:
+        args = (dtype, lens, 0.125, *_inputs(dtype, 64, lens, DATA[0]))
+        plain, corrected = (_worst(*args, _emulated(*args, c)) for c in (False, True))
+        assert max(corrected.values()) <= 1 < min(plain["dq"], plain["delta"]), (lens, plain, corrected)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("lens", LENS)
+@pytest.mark.parametrize("shared", [True, False])
+def test_gradients_do_not_lose_what_the_output_rounds_away(request, shared, lens, dtype, d):
+    """One length and ragged ones on both sides of a chunk's and a tile's end, keys shared among workgroups and not."""
+    import torch
+    if shared:
+        request.getfixturevalue("workspace")
+    else:
+        B.tir_set_workspace(None)
+    for data in DATA:
+        q, k, v, do = _inputs(dtype, d, lens, data)
+        kv = torch.stack((k, v), 2)
+        for b, n in enumerate(lens):
+            kv[b, n:] = float("nan")
+        got = _forward_and_backward(q, kv, do, lens, 0.125, dtype)
+        worst = _worst(dtype, lens, 0.125, q, k, v, do, got)
+        print(f"[case] {dtype} d={d} lens={lens} shared={shared} data={data}: worst of the tolerance {worst}", flush=True)
+        assert max(worst.values()) <= 1, worst
+        for b, n in enumerate(lens):
+            assert torch.all(got["dk"][b, n:] == 0) and torch.all(got["dv"][b, n:] == 0)
