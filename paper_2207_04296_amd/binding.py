@@ -47,12 +47,13 @@ class KvCache(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("table", ctypes.c_void_p),
                 ("blocks", ctypes.c_int64), ("heads", ctypes.c_int64), ("block_tokens", ctypes.c_int64), ("d", ctypes.c_int64), ("sequences", ctypes.c_int64), ("columns", ctypes.c_int64),
                 ("dtype", ctypes.c_int32)]
+    on_host = False      # of host tensors, whose addresses no operator takes
 
 
 def make_kv_cache(k, v, k_scale, v_scale, table):
     """tir_kv_cache of tensors: k [blocks, heads, block_tokens, d] and v [blocks, heads, d, block_tokens] of torch.int8 or torch.float8_e4m3fn,
     k_scale and v_scale [blocks, heads] float32, table [sequences, columns] int32.  The operators change k, v and the scales in place; the tensors may be changed between
-    calls (a table's entries as blocks are handed out), but not replaced."""
+    calls (a table's entries as blocks are handed out), but not replaced.  A cache of host tensors can be made and looked at; the operators refuse it."""
     import torch
     blocks, heads, tokens, d = k.shape
     want = [("k", k, (blocks, heads, tokens, d), k.dtype), ("v", v, (blocks, heads, d, tokens), k.dtype), ("k_scale", k_scale, (blocks, heads), torch.float32),
@@ -65,6 +66,7 @@ def make_kv_cache(k, v, k_scale, v_scale, table):
         raise ValueError(f"k and v: torch.int8 or torch.float8_e4m3fn is needed, got {k.dtype}")
     cache = KvCache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), table.data_ptr(), blocks, heads, tokens, d, table.shape[0], table.shape[1], codes[k.dtype])
     cache.tensors = (k, v, k_scale, v_scale, table)
+    cache.on_host = not k.is_cuda
     return cache
 
 
@@ -436,24 +438,41 @@ def _cache_arg(cache):
     return None if cache is None else ctypes.byref(cache)
 
 
+def _check_cache_call(cache, batch, lengths, count):
+    """The kernels read device memory, and an element of either array per sequence."""
+    if getattr(cache, "on_host", False):
+        raise ValueError("the cache's tensors are on the host")
+    _check_elements("start or lens", lengths, batch)
+    _check_elements("count", count, batch)
+
+
+def _check_elements(name, t, n):
+    if t is not None and not isinstance(t, int) and t.numel() < n:
+        raise ValueError(f"{name}: at least {n} elements are needed, got a tensor of {tuple(t.shape)}")
+
+
 def tir_cache_append_status(cache, K, V, start, count, batch, T, k_bs, k_rs, k_hs, v_bs, v_rs, v_hs, in_dtype, stream=0) -> int:
+    _check_cache_call(cache, batch, start, count)
     return lib().tir_cache_append(_cache_arg(cache), _ptr(K), _ptr(V), _ptr(start), _ptr(count), batch, T, k_bs, k_rs, k_hs, v_bs, v_rs, v_hs, _code(in_dtype), stream)
 
 
 def tir_cache_append(cache, K, V, start, count, batch, T, k_bs, k_rs, k_hs, v_bs, v_rs, v_hs, in_dtype, stream=None) -> None:
     """Token t of sequence b to position start[b] + t of its blocks; start and count (None: T each): int32 device tensors [batch]."""
+    _check_cache_call(cache, batch, start, count)
     st = (_native or _load_native()).tir_cache_append(cache, K, V, start, count, batch, T, k_bs, k_rs, k_hs, v_bs, v_rs, v_hs, in_dtype, stream)
     if st:
         _check(st)
 
 
 def tir_cache_attention_status(Q, cache, O, lens, count, batch, T, Hq, q_bs, q_rs, q_hs, o_bs, o_rs, o_hs, scale, in_dtype, out_dtype, stream=0) -> int:
+    _check_cache_call(cache, batch, lens, count)
     return lib().tir_cache_attention(_ptr(Q), _cache_arg(cache), _ptr(O), _ptr(lens), _ptr(count), batch, T, Hq, q_bs, q_rs, q_hs, o_bs, o_rs, o_hs, float(scale),
                                      _code(in_dtype), _code(out_dtype), stream)
 
 
 def tir_cache_attention(Q, cache, O, lens, count, batch, T, Hq, q_bs, q_rs, q_hs, o_bs, o_rs, o_hs, scale, in_dtype, out_dtype, stream=None) -> None:
     """The newest count[b] (None: T) of the lens[b] tokens of sequence b over the cache, each up to its own position."""
+    _check_cache_call(cache, batch, lens, count)
     st = (_native or _load_native()).tir_cache_attention(Q, cache, O, lens, count, batch, T, Hq, q_bs, q_rs, q_hs, o_bs, o_rs, o_hs, scale, in_dtype, out_dtype, stream)
     if st:
         _check(st)
@@ -461,6 +480,8 @@ def tir_cache_attention(Q, cache, O, lens, count, batch, T, Hq, q_bs, q_rs, q_hs
 
 def tir_cross_attention_status(Q, K, V, O, lse, lens, batch, M, N, Hq, Hkv, d, q_bs, q_rs, q_hs, k_bs, k_rs, k_hs, v_bs, v_rs, v_hs, o_bs, o_rs, o_hs, scale,
                                in_dtype, out_dtype, stream=0) -> int:
+    _check_elements("lens", lens, batch)
+    _check_elements("lse", lse, batch * Hq * M)
     return lib().tir_cross_attention(_ptr(Q), _ptr(K), _ptr(V), _ptr(O), _ptr(lse), _ptr(lens), batch, M, N, Hq, Hkv, d, q_bs, q_rs, q_hs, k_bs, k_rs, k_hs, v_bs, v_rs, v_hs,
                                      o_bs, o_rs, o_hs, float(scale), _code(in_dtype), _code(out_dtype), stream)
 
@@ -468,6 +489,8 @@ def tir_cross_attention_status(Q, K, V, O, lse, lens, batch, M, N, Hq, Hkv, d, q
 def tir_cross_attention(Q, K, V, O, lse, lens, batch, M, N, Hq, Hkv, d, q_bs, q_rs, q_hs, k_bs, k_rs, k_hs, v_bs, v_rs, v_hs, o_bs, o_rs, o_hs, scale,
                         in_dtype, out_dtype, stream=None) -> None:
     """M queries per sequence over lens[b] (None: N) keys of another one; lse (or None): fp32 [batch, Hq, M], for the backward pass."""
+    _check_elements("lens", lens, batch)
+    _check_elements("lse", lse, batch * Hq * M)
     st = (_native or _load_native()).tir_cross_attention(Q, K, V, O, lse, lens, batch, M, N, Hq, Hkv, d, q_bs, q_rs, q_hs, k_bs, k_rs, k_hs, v_bs, v_rs, v_hs,
                                                          o_bs, o_rs, o_hs, scale, in_dtype, out_dtype, stream)
     if st:
@@ -493,6 +516,9 @@ def _gradient_strides(dO, shape, o_strides, g_strides, scale, in_dtype, stream):
 def tir_cross_attention_backward_status(Q, K, V, O, dO, lse, lens, dQ, dK, dV, delta, batch, M, N, Hq, Hkv, d, q_bs, q_rs, q_hs, k_bs, k_rs, k_hs, v_bs, v_rs, v_hs,
                                         o_bs, o_rs, o_hs, g_bs=None, g_rs=None, g_hs=None, scale=None, in_dtype=None, stream=0) -> int:
     g_bs, g_rs, g_hs, scale, in_dtype, stream = _gradient_strides(dO, (batch, M, Hq, d), (o_bs, o_rs, o_hs), (g_bs, g_rs, g_hs), scale, in_dtype, stream)
+    _check_elements("lens", lens, batch)
+    _check_elements("lse", lse, batch * Hq * M)
+    _check_elements("delta", delta, batch * Hq * M)
     return lib().tir_cross_attention_backward(*[_ptr(t) for t in (Q, K, V, O, dO, lse, lens, dQ, dK, dV, delta)], batch, M, N, Hq, Hkv, d, q_bs, q_rs, q_hs, k_bs, k_rs, k_hs,
                                               v_bs, v_rs, v_hs, o_bs, o_rs, o_hs, g_bs, g_rs, g_hs, float(scale), _code(in_dtype), stream)
 
@@ -502,6 +528,9 @@ def tir_cross_attention_backward(Q, K, V, O, dO, lse, lens, dQ, dK, dV, delta, b
     """Gradients of tir_cross_attention; dQ, dK, dV with the strides of Q, K, V, dO with its own: g_bs, g_rs, g_hs, or none of the three and scale, in_dtype (and stream) right behind o_hs, for the
     strides of a tensor dO [batch, M, Hq, d] as they are (of an address: those of O); delta: fp32 scratch [batch, Hq, M]."""
     g_bs, g_rs, g_hs, scale, in_dtype, stream = _gradient_strides(dO, (batch, M, Hq, d), (o_bs, o_rs, o_hs), (g_bs, g_rs, g_hs), scale, in_dtype, stream)
+    _check_elements("lens", lens, batch)
+    _check_elements("lse", lse, batch * Hq * M)
+    _check_elements("delta", delta, batch * Hq * M)
     st = (_native or _load_native()).tir_cross_attention_backward(Q, K, V, O, dO, lse, lens, dQ, dK, dV, delta, batch, M, N, Hq, Hkv, d, q_bs, q_rs, q_hs, k_bs, k_rs, k_hs,
                                                                   v_bs, v_rs, v_hs, o_bs, o_rs, o_hs, g_bs, g_rs, g_hs, scale, in_dtype, stream)
     if st:
