@@ -88,7 +88,7 @@ __global__ void __launch_bounds__(kTokenWaves * 64) cross_token_kernel(const Cro
 #pragma unroll
         for (int u = 0; u < NL; ++u) {
             const int key = (c_first + i * KG) * CK + u * KPL + key_of;
-            const unsigned at = (unsigned)(key < n ? key : n - 1);      // (one that is there again where there is none: it gets no weight)
+            const unsigned at = (unsigned)(key < n ? key : n - 1);      // (one that is there again where there is none: it gets no weight, and step clears its value)
             c.k[u] = *(const u32x4*)(Kb + (unsigned long long)at * k_rs);
             c.v[u] = *(const u32x4*)(Vb + (unsigned long long)at * v_rs);
         }
@@ -106,8 +106,13 @@ __global__ void __launch_bounds__(kTokenWaves * 64) cross_token_kernel(const Cro
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[r][e] = 0.f;
     }
-    auto step = [&](int i, const Chunk& c) __attribute__((always_inline)) {
+    auto step = [&](int i, Chunk& c) __attribute__((always_inline)) {
         const int left = n - (c_first + i * KG) * CK - key_of;      // load u has a key of this lane's if u * KPL < left
+        if ((c_first + i * KG + 1) * CK > n) {                      // (an infinite or NaN value times a weight of zero is NaN)
+#pragma unroll
+            for (int u = 0; u < NL; ++u)
+                if (u * KPL >= left) c.v[u] = u32x4{0, 0, 0, 0};
+        }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             float t[NL];
