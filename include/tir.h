@@ -304,7 +304,7 @@ const char* tir_last_error(void);
  * buffers of their own);
  * ws = NULL removes the registration (later launches on `stream` run unsplit).  Two streams that may run at the
  * same time need two buffers: launches that share one race.  Operators that threads call on one stream take turns at
- * its buffer.  Tuning calls use the workspace of the stream they
+ * its buffer, and so do the split trials of tuning calls, which use the workspace of the stream they
  * are given and try split reductions only if it has one.
  * Errors: TIR_ERR_INVALID_ARG (buffer too small), TIR_ERR_ALIGNMENT, TIR_ERR_LAUNCH; the previous
  * registration stays in place then.
@@ -365,15 +365,15 @@ const char* tir_conv2d_transpose_variant(int64_t N, int64_t H, int64_t W, int64_
  * tir_tune_batch_matmul / tir_tune_conv2d take the arguments of tir_batch_matmul_fused / tir_conv2d_fused
  * (batch = 1 with zero batch strides tunes tir_gemm; ep may be NULL), launch every compiled variant that computes this problem
  * - and, where few tiles face a long reduction and `stream` has a registered workspace, the same variant with the
- * reduction split over 2, 3, 4, 6 or 8 workgroups per tile - `reps` times on `stream`, time those within 10 % of the fastest five more
+ * reduction split over 2, 3, 4, 6 or 8 workgroups per tile - `reps` times, time those within 10 % of the fastest five more
  * times in turn (each keeps its fastest round; a copy ring of three or more slots wins over a two-slot ring that is less than 2 % faster, the
  * trials' operands being warm in the caches), and record the winner under the problem's signature (dtypes, copy
  * modes implied by strides and alignment, extents, convolution geometry).  Later calls of the
  * operator entry points with the same signature use the recorded variant instead of the built-in
  * scoring rule.  Unlike every other call these BLOCK until the trial launches have finished, create
  * and destroy HIP events and graphs (each trial is a captured graph of `reps` launches, so that short
- * kernels are timed at the device's rate; with stream = NULL the trials run on a temporary stream
- * after a device synchronisation), and must not be called during stream capture.  The output buffer ends
+ * kernels are timed at the device's rate, on a temporary stream once the work queued on `stream` has finished), and
+ * must not be called during stream capture.  Other threads may launch on `stream` meanwhile.  The output buffer ends
  * up holding the operator's result (every variant computes the same values up to summation order).
  * *best_us (may be NULL) receives the winner's time per launch in microseconds (0 for empty problems).
  * reps must be in [1, 1000].

@@ -994,23 +994,15 @@ static tir_status plan_conv(bool need_ptrs, const void* x, const void* w, void* 
     return plan_conv_geom(need_ptrs, x, w, y, g, in, out, ep, sl, plan);
 }
 
-// Give a plan with a split reduction the workspace registered for its stream (the plan was made with that stream's
-// limits; should the registration have gone meanwhile, the same variant runs unsplit).
-static tir_status attach_workspace(Plan* plan, hipStream_t stream, StreamWorkspace* held = nullptr) {
-    if (held && plan->v && plan->p.ksplit > 1) *held = stream_workspace(stream);
-    if (!plan->v || plan->p.ksplit <= 1) return TIR_OK;
-    int dev = 0;
-    hipError_t e = hipGetDevice(&dev);
-    if (e != hipSuccess) return fail(TIR_ERR_LAUNCH, "hipGetDevice failed: %s", hipGetErrorString(e));
-    std::lock_guard<std::mutex> lock(g_ws_mu);
-    auto it = g_ws.find(std::make_pair(dev, stream));
-    if (it == g_ws.end()) {
-        plan->p.ksplit = 1;
-        return TIR_OK;
-    }
-    plan->p.ws = it->second.partial;
-    plan->p.ws_count = it->second.count;
-    return TIR_OK;
+// Give a plan with a split reduction the workspace registered for its stream, which is the caller's as long as the returned object lives (the plan was made with
+// that stream's limits; should the registration have gone meanwhile, the same variant runs unsplit).
+static StreamWorkspace attach_workspace(Plan* plan, hipStream_t stream) {
+    if (!plan->v || plan->p.ksplit <= 1) return StreamWorkspace{};
+    StreamWorkspace ws = stream_workspace(stream);
+    if (!ws.partial) plan->p.ksplit = 1;
+    plan->p.ws = ws.partial;
+    plan->p.ws_count = ws.count;
+    return ws;
 }
 
 static tir_status run(const Plan& plan, hipStream_t stream) {
@@ -1034,9 +1026,7 @@ static tir_status run(const Plan& plan, hipStream_t stream) {
 }
 
 static tir_status launch(Plan& plan, hipStream_t stream) {
-    StreamWorkspace held = {};
-    tir_status st = attach_workspace(&plan, stream, &held);
-    if (st != TIR_OK) return st;
+    const StreamWorkspace held = attach_workspace(&plan, stream);
     return run(plan, stream);
 }
 
@@ -1073,21 +1063,27 @@ static tir_status tune_problem(MakePlan make_plan, int reps, hipStream_t stream,
         (void)hipEventDestroy(e0);
         return fail(TIR_ERR_LAUNCH, "hipEventCreate failed: %s", hipGetErrorString(ce));
     }
-    // the legacy default stream cannot be captured: trials then run on a stream of their own (which borrows the
-    // caller's stream's workspace: everything queued there has finished, and the trials finish before the call returns)
+    // The trials are captured on a stream of their own: the legacy default stream cannot be captured, and what another thread launches on a stream that is being
+    // captured ends up in the graph.  Work already queued on the caller's stream comes first.
     const hipStream_t caller_stream = stream;
     hipStream_t own = nullptr;
-    if (!stream) {
-        ce = hipStreamCreateWithFlags(&own, hipStreamNonBlocking);
-        if (ce == hipSuccess) ce = hipDeviceSynchronize();      // work already queued on the default stream comes first
-        if (ce != hipSuccess) {
-            (void)hipEventDestroy(e0);
-            (void)hipEventDestroy(e1);
-            if (own) (void)hipStreamDestroy(own);
-            return fail(TIR_ERR_LAUNCH, "tuning: cannot create a stream: %s", hipGetErrorString(ce));
-        }
-        stream = own;
+    ce = hipStreamCreateWithFlags(&own, hipStreamNonBlocking);
+    if (ce == hipSuccess) ce = stream ? hipStreamSynchronize(stream) : hipDeviceSynchronize();
+    if (ce != hipSuccess) {
+        (void)hipEventDestroy(e0);
+        (void)hipEventDestroy(e1);
+        if (own) (void)hipStreamDestroy(own);
+        return fail(TIR_ERR_LAUNCH, "tuning: cannot create a stream: %s", hipGetErrorString(ce));
     }
+    stream = own;
+    // Split trials borrow the workspace of the caller's stream: in turn with the operators that other threads call there, and once what these have queued has finished.
+    // The trials finish before the turn ends.
+    auto borrow = [&](Plan* pl, StreamWorkspace* held) -> tir_status {
+        *held = attach_workspace(pl, caller_stream);
+        if (!held->partial) return TIR_OK;
+        const hipError_t e = hipStreamSynchronize(caller_stream);
+        return e == hipSuccess ? TIR_OK : fail(TIR_ERR_LAUNCH, "tuning: waiting for the stream failed: %s", hipGetErrorString(e));
+    };
     TrialGuard guard;
     Choice best = kNoChoice;
     float best_ms = 0.f;
@@ -1124,7 +1120,7 @@ static tir_status tune_problem(MakePlan make_plan, int reps, hipStream_t stream,
         st = timed_plan(base, reps, &best_ms);
         (void)hipEventDestroy(e0);
         (void)hipEventDestroy(e1);
-        if (own) (void)hipStreamDestroy(own);
+        (void)hipStreamDestroy(own);
         if (st == TIR_OK) {
             if (best_us) *best_us = (double)best_ms * 1e3;
             if (best_name) *best_name = base.v->name;
@@ -1142,7 +1138,8 @@ static tir_status tune_problem(MakePlan make_plan, int reps, hipStream_t stream,
         Plan pl;
         st = make_plan(&pl);
         if (st == TIR_ERR_UNSUPPORTED) { st = TIR_OK; continue; }      // this variant cannot run the problem
-        if (st == TIR_OK) st = attach_workspace(&pl, caller_stream);
+        StreamWorkspace held = {};
+        if (st == TIR_OK) st = borrow(&pl, &held);
         if (st != TIR_OK) break;
         if (pl.p.ksplit != ks) continue;              // this split does not apply
         if (ks > 1) {
@@ -1174,7 +1171,8 @@ static tir_status tune_problem(MakePlan make_plan, int reps, hipStream_t stream,
                 g_trial = t.first;
                 Plan pl;
                 st = make_plan(&pl);
-                if (st == TIR_OK) st = attach_workspace(&pl, caller_stream);
+                StreamWorkspace held = {};
+                if (st == TIR_OK) st = borrow(&pl, &held);
                 float ms = 0.f;
                 if (st == TIR_OK) st = timed_plan(pl, reps, &ms);
                 if (st != TIR_OK) break;
@@ -1201,7 +1199,7 @@ static tir_status tune_problem(MakePlan make_plan, int reps, hipStream_t stream,
     }
     (void)hipEventDestroy(e0);
     (void)hipEventDestroy(e1);
-    if (own) (void)hipStreamDestroy(own);
+    (void)hipStreamDestroy(own);
     if (st != TIR_OK) return st;
     if (best.v) {
         std::lock_guard<std::mutex> lock(g_tune_mu);
