@@ -236,7 +236,7 @@ tir_status tir_cache_append(const tir_kv_cache* cache, const void* K, const void
  * lens[b] - count[b] + t and sees the positions up to its own:
  *     O[b,t,hq] = sum_j p_j * v_j,  p = softmax over j of scale * (q[b,t,hq] . k_j),  k_j and v_j of key head hq / (Hq / heads)
  * Q[b*q_bs + t*q_rs + hq*q_hs + c], O alike; heads must divide Hq.  Positions in blocks that are not there are not seen; a query that sees nothing
- * gives zeros.  Rows t >= count[b] of O are left as they were.  in = F16 or BF16; out = the same type or F32.  scale must be finite.
+ * gives zeros.  Rows t >= count[b] of O are left as they were.  in = F16 or BF16; out = the same type or F32.  scale must be finite, and at most 2^127 in magnitude.
  * Scores, softmax and sums are fp32; the 8-bit numbers enter the products unrounded; a probability times the scale of its values is rounded to the input type
  * relative to the row's largest.  |O - exact| <= 2e-3 * T + 1e-5 with F16, 6e-3 * T + 1e-5 with BF16 (plus 2^-8 * |O| for BF16 output), T = sum_j p_j |v_j|, as for tir_attention.
  * With a workspace registered for `stream` (tir_set_workspace) few queries over many keys are shared among workgroups, whose results are added in a fixed order; without one
@@ -254,7 +254,7 @@ tir_status tir_cache_attention(const void* Q, const tir_kv_cache* cache, void* O
  *     O[b,i,hq] = sum_j p_j * V[b,j,hk],  p = softmax over j < lens[b] of scale * (Q[b,i,hq] . K[b,j,hk]),  hk = hq / (Hq / Hkv)
  * Q[b*q_bs + i*q_rs + hq*q_hs + c], c < d, and likewise K, V (by hk) and O; Hkv must divide Hq, d is 64 or 128.  Keys and values from lens[b] on are not used, whatever they
  * hold.  A sequence without keys gives zeros.  lse: fp32 [batch][Hq][M], dense, log(sum_j exp(scale * Q.K)), -infinity without keys, which the backward pass
- * needs; NULL where it is not wanted.  in = F16 or BF16; out = the same type or F32.  Arithmetic and accuracy as tir_attention; lse to 1e-5 + 2^-22 * max|scale * Q.K|.
+ * needs; NULL where it is not wanted.  in = F16 or BF16; out = the same type or F32; scale as for tir_cache_attention.  Arithmetic and accuracy as tir_attention; lse to 1e-5 + 2^-22 * max|scale * Q.K|.
  * With a workspace registered for `stream` few queries over many keys are shared among workgroups, whose results are added in a fixed order.
  * Pointers 16-byte aligned, all strides multiples of 8 elements, row strides at most 2^23, N at most 2^31 - 2^16; the strides of O must keep its rows apart, those of the inputs may be 0.  batch, M or Hq = 0 is a no-op.
  */

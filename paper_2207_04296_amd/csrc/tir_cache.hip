@@ -167,7 +167,8 @@ tir_status tir_cache_attention(const void* Q, const tir_kv_cache* cache, void* O
     if (st == TIR_OK) st = check_row_strides(who, "Q", q_bs, q_rs, q_hs);
     if (st == TIR_OK) st = check_row_strides(who, "O", o_bs, o_rs, o_hs);
     if (st != TIR_OK) return st;
-    if (!(scale == scale) || scale > 3.0e38f || scale < -3.0e38f) return host_error(TIR_ERR_INVALID_ARG, "%s: scale must be finite", who);
+    st = check_scale(who, scale);
+    if (st != TIR_OK) return st;
     if (Hq % p.c.heads) return host_error(TIR_ERR_INVALID_ARG, "%s: %d key heads do not divide %lld query heads", who, p.c.heads, (long long)Hq);
     if (batch == 0 || T == 0 || Hq == 0) return TIR_OK;
     if (!Q || !O || !lens) return host_error(TIR_ERR_INVALID_ARG, "%s: Q, O or lens is null", who);

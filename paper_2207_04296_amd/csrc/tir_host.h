@@ -43,12 +43,19 @@ inline tir_status check_row_strides(const char* who, const char* what, int64_t b
     return TIR_OK;
 }
 
+// The kernels multiply by scale * log2(e), which has to be finite too.
+inline tir_status check_scale(const char* who, float scale) {
+    if (!(scale <= 0x1p127f && scale >= -0x1p127f)) return host_error(TIR_ERR_INVALID_ARG, "%s: scale must be finite and at most 2^127 in magnitude", who);
+    return TIR_OK;
+}
+
 // Extents of the attention over another sequence's states, forward and backward.
 inline tir_status check_cross(const char* who, int64_t batch, int64_t M, int64_t N, int64_t Hq, int64_t Hkv, int64_t d, float scale) {
     if (batch < 0 || M < 0 || N < 0 || Hq < 0 || Hkv < 1 || d < 0)
         return host_error(TIR_ERR_INVALID_ARG, "%s: negative extent or no key head (batch=%lld M=%lld N=%lld Hq=%lld Hkv=%lld d=%lld)", who, (long long)batch, (long long)M, (long long)N, (long long)Hq, (long long)Hkv, (long long)d);
     if (d != 64 && d != 128) return host_error(TIR_ERR_UNSUPPORTED, "%s: head dimension %lld (64 and 128 are compiled)", who, (long long)d);
-    if (!(scale == scale) || scale > 3.0e38f || scale < -3.0e38f) return host_error(TIR_ERR_INVALID_ARG, "%s: scale must be finite", who);
+    const tir_status st = check_scale(who, scale);
+    if (st != TIR_OK) return st;
     if (Hq % Hkv) return host_error(TIR_ERR_INVALID_ARG, "%s: %lld key heads do not divide %lld query heads", who, (long long)Hkv, (long long)Hq);
     if (batch > kMax31 || M > kMax31 || N > kMax31 - 65535 || Hq > kMax31) return host_error(TIR_ERR_UNSUPPORTED, "extent beyond 2^31-1");
     if (batch == 0 || Hq == 0) return TIR_OK;

@@ -73,3 +73,12 @@ def test_arrays_that_are_long_enough_pass():
     for n in (2, 3, 70):
         assert B.tir_cache_append_status(_cache(), X + 2, X, Long(n), Long(n), 2, 1, *S, *S, "f16") == B.TIR_ERR_ALIGNMENT
         assert B.tir_cross_attention_status(X, X + 2, X, X, Long(2, 2, n), Long(n), 2, 2, 3, 2, 2, 64, *S, *S, *S, *S, 0.1, "f16", "f16") == B.TIR_ERR_ALIGNMENT
+
+
+@pytest.mark.parametrize("scale", [2.0 ** 127 * (1 + 2.0 ** -20), 2.5e38, -2.5e38])
+def test_a_scale_whose_exponent_overflows_is_refused(scale):
+    """scale * log2(e) would be infinite, and a score of zero NaN; 2^127 itself passes (and is refused for what is not aligned)."""
+    for s, status in ((scale, B.TIR_ERR_INVALID_ARG), (2.0 ** 127, B.TIR_ERR_ALIGNMENT), (-2.0 ** 127, B.TIR_ERR_ALIGNMENT)):
+        assert B.tir_cache_attention_status(X + 2, _cache(), X, X, X, 2, 1, 2, *S, *S, s, "f16", "f16") == status and B.last_error()
+        assert B.tir_cross_attention_status(X + 2, X, X, X, X, X, 2, 1, 3, 2, 2, 64, *S, *S, *S, *S, s, "f16", "f16") == status
+        assert B.tir_cross_attention_backward_status(X + 2, X, X, X, X, X, X, X, X, X, X, 2, 1, 3, 2, 2, 64, *S, *S, *S, *S, *S, s, "f16") == status
