@@ -47,6 +47,10 @@ hipError_t launch_cache_attention(const CacheAttnParams& p, int dt, int ct, int 
 //
 // Tiles of 32 rows and of 256, us: 4 x 509 tokens x 32 query heads (8 key heads) of 128 over 4 thousand, e4m3 176 / 148, int8 and bf16 203 / 150, heads of 64 112 / 99; from fewer rows or workgroups the
 // small ones are as fast or faster: 1000 tokens over themselves 34.9 / 39.4, 64 x 20 tokens over 2500 139 / 187, 16 x 200 x 16 heads of 64 over 1200 42 / 56.
+//
+// A table much wider than the sequences lets the 256-row tiles count slices that then have no keys.  130 tokens x 16 query heads (4 key heads) of 128 in a table of 200 000 positions, tiles of 32 and of 256, us:
+// holding 130 6.3 / 14.1, 1000 15.0 / 19.1, 4000 25.3 / 26.5, 16 000 56.0 / 46.0, 200 000 541 / 344.  The columns do not tell these apart; what a wide table costs a short prompt is less than what narrow tiles cost a
+// long one.  Single tokens gain from it: 1 x 777 x 8 heads of 64 7.1 us in a table of its length, 6.4 in a wide one (one chunk per wave instead of two).
 static void choose_cache_kernel(CacheAttnParams* p, int64_t d, const StreamWorkspace& ws) {
     const int64_t heads = (int64_t)p->batch * p->c.heads, rows = (int64_t)p->T * p->G, keys = (int64_t)p->c.cols << p->c.shift;
     const int64_t part = d == 64 ? cache_partial_bytes<64>() : cache_partial_bytes<128>();

@@ -103,6 +103,8 @@ tir_status tir_cross_attention(const void* Q, const void* K, const void* V, void
         }
     };
     hipError_t e;
+    // The vector kernel's time grows with the rows, that of a tile of 64 does not.  8 x 1500 keys x 16 heads of 64, 1, 2, 4, 5, 6 and 8 rows, us: 13.6, 14.5, 17.6, 20.7, 23.3, 28.4, and the tile 17.0 for 2 to 16;
+    // x 8 heads of 128: 12.9, 13.9, 18.4, 21.3, 23.6, 28.9, and 19.0; 100 000 keys x 4 heads of 128, 4, 5 and 8 rows: 57, 70, 98, and 85.
     if (p.M <= kTokenRows && N > 0) {
         const int64_t chunk = d == 64 ? 32 : 16;         // two per wave
         share(p.batch, 256 / p.batch, N / (8 * chunk), d == 64 ? cross_token_partial<64>(p.M) : cross_token_partial<128>(p.M));
