@@ -296,6 +296,7 @@ __global__ void __launch_bounds__(kGradThreads, 2) grad_rows_kernel(const GradPa
         }
     }
     const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    float first = 0.f;                                 // dP of the row's first key: D is summed from it on, and a single key's D is its dP to the bit, as its dS of zero has to be
     if (FEW && chunks > 0) {
         copy_barrier<0>();
 #pragma unroll 1
@@ -305,11 +306,13 @@ __global__ void __launch_bounds__(kGradThreads, 2) grad_rows_kernel(const GradPa
             for (int ks = 0; ks < KSTEPS; ++ks) s = InTraits<DT>::mfma(T::along(smem, jb * 32, ks, l31, g), qf[ks], ks == 0 ? zero16 : s);
 #pragma unroll
             for (int ks = 0; ks < KSTEPS; ++ks) dp = InTraits<DT>::mfma(T::along(smem + T::BYTES, jb * 32, ks, l31, g), of[ks], ks == 0 ? zero16 : dp);
+            if (jb == 0) first = __shfl(dp[0], l31);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) delta += jb * 32 + 8 * (r >> 2) + 4 * g + (r & 3) < n ? __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], p.scale_log2e, -lse2)) * dp[r] : 0.f;
+            for (int r = 0; r < 16; ++r) delta += jb * 32 + 8 * (r >> 2) + 4 * g + (r & 3) < n ? __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], p.scale_log2e, -lse2)) * (dp[r] - first) : 0.f;
         }
     }
     delta += __shfl_xor(delta, 32);
+    if (FEW) delta += first;
 
     f32x16 acc[DB], pk[FEW ? 1 : DB];                  // sums of dS' K and of P K
 #pragma unroll
@@ -383,7 +386,7 @@ __global__ void __launch_bounds__(kGradThreads, 2) grad_rows_kernel(const GradPa
             TIR_FENCE();                       // (the next block's operands read ahead of here would not fit the registers)
         }
     }
-    const float f = p.scale * pf / by;
+    const float f = !FEW && n == 1 ? 0.f : p.scale * pf / by;      // (a single key's dS is zero, which the rounding of an estimate would not leave)
     e_sum = (e_sum + __shfl_xor(e_sum, 32)) * pf;
     const bool whole = FEW || p.slices == 1;
     if (live && g == 0 && (whole || blockIdx.y == 0)) {
@@ -393,7 +396,7 @@ __global__ void __launch_bounds__(kGradThreads, 2) grad_rows_kernel(const GradPa
         const int mr = (int)fastdiv((unsigned)r, p.div_g_magic, p.div_g_shift);
         p.delta[((long long)b * p.heads * p.G + h * p.G + r - mr * p.G) * p.M + mr] = whole ? delta + e_sum : delta;
     }
-    const float fp = -(p.scale * pf) * e_sum;
+    const float fp = !FEW && n == 1 ? 0.f : -(p.scale * pf) * e_sum;
     if constexpr (!FEW) {
         if (p.slices > 1) {
             if (wave * 32 >= rows) return;               // (nobody reads these)
@@ -401,7 +404,7 @@ __global__ void __launch_bounds__(kGradThreads, 2) grad_rows_kernel(const GradPa
             typedef float f32x4 __attribute__((ext_vector_type(4)));
             float* const part = p.ws + ((long long)blockIdx.x * p.slices + blockIdx.y) * grad_partial(false, DH);
             f32x4* const o = (f32x4*)part + wave * (32 * DH / 4) + lane;
-            const float fk = p.scale * pf;
+            const float fk = n == 1 ? 0.f : p.scale * pf;
 #pragma unroll
             for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -582,7 +585,7 @@ __global__ void __launch_bounds__(kGradThreads * RG, DH == 64 && RG == 1 ? 3 : 2
         }
     }
     const float pf = DT == DT_F16 ? 0x1p-14f : 1.f;
-    const float fk = p.scale * pf / by, fv = pf;         // (dS was formed from probabilities times their factor)
+    const float fk = n == 1 ? 0.f : p.scale * pf / by, fv = pf;      // (dS was formed from probabilities times their factor; that of a single key is zero)
     if constexpr (RG > 1) {
         __syncthreads();                                 // the rings are free
         f32x4* const o = (f32x4*)(smem + wave * MERGE) + lane;

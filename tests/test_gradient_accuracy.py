@@ -102,3 +102,21 @@ def test_gradients_do_not_lose_what_the_output_rounds_away(request, shared, lens
         assert max(worst.values()) <= 1, worst
         for b, n in enumerate(lens):
             assert torch.all(got["dk"][b, n:] == 0) and torch.all(got["dv"][b, n:] == 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("lens", [[1], [1, 1, 1], [1, 40, 1], [70, 1, 0], [1, 300]])
+def test_a_single_key_has_no_gradient(workspace, lens, dtype, d):  # noqa: F811
+    """The probability of a single key is 1 whatever the query: dQ and dK of such a sequence are zero exactly, and dV is the sum of dO (rounded once: u of itself; a P within 1e-5 of 1
+    rounds to 1, and fp32 sums of up to 50 terms are within 1e-5 of their magnitudes)."""
+    import torch
+    q, k, v, do = _inputs(dtype, d, lens, DATA[1])
+    got = _forward_and_backward(q, torch.stack((k, v), 2), do, lens, 0.3, dtype)
+    print(f"[case] single keys, {dtype} d={d} lens={lens}", flush=True)
+    for b, n in enumerate(lens):
+        if n == 1:
+            assert torch.all(got["dq"][b] == 0) and torch.all(got["dk"][b] == 0)
+            want, mag = do[b].double().sum(0), do[b].double().abs().sum(0)
+            assert torch.all((got["dv"][b, 0].double() - want).abs() <= U[dtype] * want.abs() + 1e-5 * mag)
