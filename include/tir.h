@@ -274,6 +274,7 @@ tir_status tir_cross_attention(const void* Q, const void* K, const void* V, void
  * dV from lens[b] on are zeros, as are the rows of dQ of a sequence without keys.  A stride of Q, K or V that is 0 along an axis of more than one is refused: the gradients would overlap
  * (the gradient of a broadcast input is the sum over what it was broadcast to); other strides have to keep their rows apart, those of O and dO may be 0.  delta: scratch of the caller's, fp32 [batch][Hq][M]; holds D afterwards.
  * Nothing is added atomically: the same call gives the same bits.  P and dS are rounded to the input type for the last products (F16: times a power of two that uses the type's range), sums are fp32.
+ * (In calls of up to 16384 pairs, batch * Hq * M * N, and up to 256 tiles of 128 keys, they are operands in two parts: u^2 stands for the u of P and dS below.)
  * D is summed from P and dO . V in fp32: dO . O, whose O was rounded, is its first estimate only, so that values far from zero cost no accuracy.  With u = 2^-11 (F16) or 2^-8 (BF16), a_ij = sum_c |dO_ic V_jc|,
  * A_i = sum_j P_ij a_ij and s_ij = 2e-5 * P_ij * (a_ij + A_i), for scores of up to a hundred, besides u of the result and F16's subnormals:
  *     |dV - exact| <= 1.05 u * sum_i P_ij |dO_i|                                  |delta - D| <= 2e-5 * A_i

@@ -16,7 +16,7 @@
 // 16-byte column c of row r is kept at column c ^ (4 * (r/2 mod 2) + r/4 mod 4): the 16 rows of a ds_read_b128 phase meet all banks once, and the 8 rows
 // whose 64-byte segments one transposing read takes lie in both halves of a 128-byte row, the least a 512-byte read can do.
 //
-// Roundings: P and dS are rounded to the input type for the last products.  BF16 has fp32's range.  In F16 a probability is held times 2^14, and dS times a power
+// Roundings: P and dS are rounded to the input type for the last products (in small calls in two parts, see kTwoParts).  BF16 has fp32's range.  In F16 a probability is held times 2^14, and dS times a power
 // of two per row (per key) that keeps the largest so far below 2^15: gradients arrive at any magnitude, and dS relative to 1 would fall among F16's subnormals where dQ does not.
 #pragma once
 #include "tir_kernel.h"
@@ -41,13 +41,18 @@ struct GradParams {
 };
 
 constexpr int kGradWaves = 4, kGradThreads = 64 * kGradWaves, kGradTile = 32 * kGradWaves;      // rows resp. keys of a workgroup
+// Pairs (query, key) of a call, all heads together, up to which P and dS are operands in two parts: a value rounded to 16 bits and what that left of it, rounded likewise.  One rounding of a
+// probability is up to u of a sum that it dominates, and as much again as the result's own rounding in the mean; over many they even out to 1.42 of it, over a few hundred they may reach 1.6 (2 x 110 keys x
+// 8 heads of 128, bf16: dV off by 2.6e-3, 1.66e-3 in two parts).  Calls this small mostly wait for memory and launches: that one takes 17.2 us instead of 16.1, 27 x 2 keys x 2 x 3 heads 12.6 instead of 12.0, one token x 500 keys x
+// 8 heads on one 24.5 instead of 22.7, 128 x 128 keys 21.2 instead of 19.1, 16 x 1 x 64 keys x 16 heads of 64 12.4 instead of 11.8.  Only where the pass over keys takes two row groups: the other form has no registers left at d = 64.
+constexpr int kTwoParts = 1 << 14;
 constexpr int kFewKeys = 64;        // up to so many keys are one chunk of the pass over rows
 
 // Partial sums of a slice, in floats.  Rows: dS' K, P K and the rows' e; keys: dK and dV.
 constexpr int grad_partial(bool keys, int d) { return 2 * kGradTile * d + (keys ? 0 : kGradTile); }
 
-hipError_t launch_grad_rows(const GradParams& p, int dt, int dh, hipStream_t stream);
-hipError_t launch_grad_keys(const GradParams& p, int dt, int dh, hipStream_t stream);
+hipError_t launch_grad_rows(const GradParams& p, int dt, int dh, bool two, hipStream_t stream);      // (two: operands in two parts)
+hipError_t launch_grad_keys(const GradParams& p, int dt, int dh, bool two, hipStream_t stream);
 
 __device__ __forceinline__ int grad_swz(int row) { return ((row & 2) << 1) | ((row >> 2) & 3); }
 
@@ -166,6 +171,23 @@ template <int DT, int DB> __device__ __forceinline__ void round_ds(f32x16& ds, f
         for (int i = 0; i < 8; ++i) w[i] = grad_pack<DT>(ds[2 * i], ds[2 * i + 1]);
     }
 }
+// What the rounding of x * by to w left of it, rounded likewise: a second operand.
+template <int DT> __device__ __forceinline__ void rest_of(const f32x16& x, float by, unsigned (&w)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float lo, hi;
+        if constexpr (DT == DT_F16) {
+            typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+            const h2 v = __builtin_bit_cast(h2, w[i]);
+            lo = (float)v[0];
+            hi = (float)v[1];
+        } else {
+            lo = __builtin_bit_cast(float, w[i] << 16);
+            hi = __builtin_bit_cast(float, w[i] & 0xffff0000u);
+        }
+        w[i] = grad_pack<DT>(__builtin_fmaf(x[2 * i], by, -lo), __builtin_fmaf(x[2 * i + 1], by, -hi));
+    }
+}
 // Four values of a row into a tile of rows in LDS, and that tile to memory in 16-byte pieces: a row's values lie in two lanes, 8 bytes at a time.  Written through (see the forward kernels);
 // `near`: the tile's rows lie within 2^31 bytes.  place(r): elements from base to row r.  Threads of the workgroup (T = its size) or of a wave (64) take part.
 template <int DH> __device__ __forceinline__ void grad_stage(char* tile, int row, int ch, uint2 v) { *(uint2*)(tile + row * (DH * 2) + ((ch * 2) ^ ((row & 7) << 4))) = v; }
@@ -214,7 +236,7 @@ template <int N, int LA, class READ, class MUL> __device__ __forceinline__ void 
 // Otherwise, at d = 128, the two sums are 128 registers and the queries 32; dO is kept in LDS, beside chunks of half as many keys.  The second sum costs a third of the matrix work and half of
 // the vector registers: both passes with and without it, 2 x 2047 x 4095 and 1365 keys x 16 / 4 heads of 128 400 and 353 us, 16 x 250 x 333 x 12 heads of 64 33.4 and 31.9 (two workgroups per CU and three).
 // ---------------------------------------------------------------------------------------------
-template <int DT, int DH, bool FEW>
+template <int DT, int DH, bool FEW, bool TWO>
 __global__ void __launch_bounds__(kGradThreads, 2) grad_rows_kernel(const GradParams p) {
     constexpr int CH = FEW || DH == 64 ? 64 : 32;      // keys of a chunk
     constexpr bool G_LDS = !FEW && DH == 128;
@@ -383,6 +405,16 @@ __global__ void __launch_bounds__(kGradThreads, 2) grad_rows_kernel(const GradPa
                     here(pk[db]);
                 }
             }
+            if constexpr (TWO) {
+                rest_of<DT>(ds, by, w);
+                products<2 * DB, LA>([&](int t) __attribute__((always_inline)) { return T::across(tk, jb * 32 + t / DB * 16, t % DB, blk, s16); },
+                                     [&](int t, const uint4& x) __attribute__((always_inline)) {
+                                         const int at = t / DB * 4;
+                                         acc[t % DB] = InTraits<DT>::mfma(x, make_uint4(w[at], w[at + 1], w[at + 2], w[at + 3]), acc[t % DB]);
+                                     });
+#pragma unroll
+                for (int db = 0; db < DB; ++db) here(acc[db]);
+            }
             TIR_FENCE();                       // (the next block's operands read ahead of here would not fit the registers)
         }
     }
@@ -444,7 +476,7 @@ __global__ void __launch_bounds__(kGradThreads, 2) grad_rows_kernel(const GradPa
 // they stay in LDS, and so they do at d = 64 with RG = 1, where 168 registers then hold three workgroups per CU instead of two: 16 x 250 x 333 x 12 heads (576 workgroups) both passes 41.0 -> 37.3 us,
 // 4 x 4096 x 577 x 8 heads 119 -> 114.
 // ---------------------------------------------------------------------------------------------
-template <int DT, int DH, int RG>
+template <int DT, int DH, int RG, bool TWO>
 __global__ void __launch_bounds__(kGradThreads * RG, DH == 64 && RG == 1 ? 3 : 2) grad_keys_kernel(const GradParams p) {
     constexpr int RB = DH == 64 ? 64 : 32;              // rows of a chunk
     typedef GradTile<DH, RB> T;
@@ -531,6 +563,21 @@ __global__ void __launch_bounds__(kGradThreads * RG, DH == 64 && RG == 1 ? 3 : 2
     const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     typedef float f32x4 __attribute__((ext_vector_type(4)));
 
+    // (w holds the first part)
+    unsigned w[8];
+    auto second_part = [&](const char* tile, int ib, const f32x16& x, float factor, f32x16 (&to)[DB]) __attribute__((always_inline)) {
+        if constexpr (TWO) {
+            rest_of<DT>(x, factor, w);
+            products<2 * DB, LA>([&](int t) __attribute__((always_inline)) { return T::across(tile, ib * 32 + t / DB * 16, t % DB, blk, s16); },
+                                 [&](int t, const uint4& y) __attribute__((always_inline)) {
+                                     const int ss = t / DB;
+                                     to[t % DB] = InTraits<DT>::mfma(y, make_uint4(w[4 * ss], w[4 * ss + 1], w[4 * ss + 2], w[4 * ss + 3]), to[t % DB]);
+                                 });
+#pragma unroll
+            for (int db = 0; db < DB; ++db) here(to[db]);
+        }
+    };
+
     for (int i = 0; i < loops; ++i) {
         copy_barrier<0>();
         if (i + 1 < mine) copy((i + 1) & 1);
@@ -543,7 +590,6 @@ __global__ void __launch_bounds__(kGradThreads * RG, DH == 64 && RG == 1 ? 3 : 2
             products<KSTEPS, LA>([&](int ks) __attribute__((always_inline)) { return T::along(tq, ib * 32, ks, l31, g); },
                                  [&](int ks, const uint4& x) __attribute__((always_inline)) { pr = InTraits<DT>::mfma(x, kf[ks], ks == 0 ? zero16 : pr); });
             // row 8*a + 4*g + e of the block is register 4*a + e.  Rows behind the last read zeros: P = 1 there, dO and dS are 0.
-            unsigned w[8];
 #pragma unroll
             for (int a = 0; a < 4; ++a) {
                 const f32x4 l4 = *(const f32x4*)(to + T::BYTES + (ib * 32 + 8 * a + 4 * g) * 4);
@@ -561,6 +607,7 @@ __global__ void __launch_bounds__(kGradThreads * RG, DH == 64 && RG == 1 ? 3 : 2
                                  });
 #pragma unroll
             for (int db = 0; db < DB; ++db) here(dv[db]);
+            second_part(to, ib, pr, 1.f, dv);
             f32x16 ds;
             if constexpr (V_LDS)
                 products<KSTEPS, LA>([&](int ks) __attribute__((always_inline)) { return TwoOperands{T::along(to, ib * 32, ks, l31, g), VT::along(smem + V_AT, wave * 32, ks, l31, g)}; },
@@ -582,6 +629,7 @@ __global__ void __launch_bounds__(kGradThreads * RG, DH == 64 && RG == 1 ? 3 : 2
                                  });
 #pragma unroll
             for (int db = 0; db < DB; ++db) here(dk[db]);
+            second_part(tq, ib, ds, by, dk);
         }
     }
     const float pf = DT == DT_F16 ? 0x1p-14f : 1.f;

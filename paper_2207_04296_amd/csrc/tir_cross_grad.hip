@@ -7,25 +7,32 @@
 
 namespace tir {
 
-template <int DT, int DH, bool KEYS> static hipError_t launch_pass(const GradParams& p, hipStream_t stream) {
+// Two groups of waves on a tile's keys where there is one workgroup per CU.
+static int keys_pass_groups(int64_t tiles, int64_t slices) { return tiles * slices <= 256 ? 2 : 1; }
+
+template <int DT, int DH, bool TWO> static hipError_t launch_rows_pass(const GradParams& p, dim3 grid, hipStream_t stream) {
+    return launch_kernel(p.N <= kFewKeys ? &grad_rows_kernel<DT, DH, true, TWO> : &grad_rows_kernel<DT, DH, false, TWO>, grid, dim3(kGradThreads), stream, p);
+}
+template <int DT, int DH, bool KEYS> static hipError_t launch_pass(const GradParams& p, bool two, hipStream_t stream) {
     const unsigned tiles = (unsigned)(p.batch * p.heads * p.tiles);
     const dim3 grid(tiles, (unsigned)p.slices);
     hipError_t e;
-    if (!KEYS) e = launch_kernel(p.N <= kFewKeys ? &grad_rows_kernel<DT, DH, true> : &grad_rows_kernel<DT, DH, false>, grid, dim3(kGradThreads), stream, p);
-    else if ((int64_t)tiles * p.slices <= 256) e = launch_kernel(&grad_keys_kernel<DT, DH, 2>, grid, dim3(2 * kGradThreads), stream, p);
-    else e = launch_kernel(&grad_keys_kernel<DT, DH, 1>, grid, dim3(kGradThreads), stream, p);
+    if (!KEYS) e = two ? launch_rows_pass<DT, DH, true>(p, grid, stream) : launch_rows_pass<DT, DH, false>(p, grid, stream);
+    else if (two) e = launch_kernel(&grad_keys_kernel<DT, DH, 2, true>, grid, dim3(2 * kGradThreads), stream, p);
+    else if (keys_pass_groups(tiles, p.slices) == 2) e = launch_kernel(&grad_keys_kernel<DT, DH, 2, false>, grid, dim3(2 * kGradThreads), stream, p);
+    else e = launch_kernel(&grad_keys_kernel<DT, DH, 1, false>, grid, dim3(kGradThreads), stream, p);
     if (e != hipSuccess || p.slices == 1) return e;
     return launch_kernel(&grad_sum_kernel<DT, DH, KEYS>, dim3((KEYS ? 2 : 1) * kGradTile * DH / 1024, tiles), dim3(256), stream, p);
 }
-template <bool KEYS> static hipError_t launch_by_type(const GradParams& p, int dt, int dh, hipStream_t stream) {
-    if (dt == DT_F16 && dh == 64) return launch_pass<DT_F16, 64, KEYS>(p, stream);
-    if (dt == DT_F16 && dh == 128) return launch_pass<DT_F16, 128, KEYS>(p, stream);
-    if (dt == DT_BF16 && dh == 64) return launch_pass<DT_BF16, 64, KEYS>(p, stream);
-    if (dt == DT_BF16 && dh == 128) return launch_pass<DT_BF16, 128, KEYS>(p, stream);
+template <bool KEYS> static hipError_t launch_by_type(const GradParams& p, int dt, int dh, bool two, hipStream_t stream) {
+    if (dt == DT_F16 && dh == 64) return launch_pass<DT_F16, 64, KEYS>(p, two, stream);
+    if (dt == DT_F16 && dh == 128) return launch_pass<DT_F16, 128, KEYS>(p, two, stream);
+    if (dt == DT_BF16 && dh == 64) return launch_pass<DT_BF16, 64, KEYS>(p, two, stream);
+    if (dt == DT_BF16 && dh == 128) return launch_pass<DT_BF16, 128, KEYS>(p, two, stream);
     return hipErrorInvalidValue;
 }
-hipError_t launch_grad_rows(const GradParams& p, int dt, int dh, hipStream_t stream) { return launch_by_type<false>(p, dt, dh, stream); }
-hipError_t launch_grad_keys(const GradParams& p, int dt, int dh, hipStream_t stream) { return launch_by_type<true>(p, dt, dh, stream); }
+hipError_t launch_grad_rows(const GradParams& p, int dt, int dh, bool two, hipStream_t stream) { return launch_by_type<false>(p, dt, dh, two, stream); }
+hipError_t launch_grad_keys(const GradParams& p, int dt, int dh, bool two, hipStream_t stream) { return launch_by_type<true>(p, dt, dh, two, stream); }
 
 // How many workgroups share a tile's walk of `steps` chunks (of 64 rows or keys): as many as the chip has room for, each with two chunks at least, as far as the partial sums fit.
 static int slices_of(int64_t tiles, int64_t room, int64_t steps, int64_t part_bytes, const StreamWorkspace& ws) {
@@ -90,14 +97,16 @@ tir_status tir_cross_attention_backward(const void* Q, const void* K, const void
     p.div_g_magic = dg.magic; p.div_g_shift = dg.shift;
     const StreamWorkspace ws = stream_workspace((hipStream_t)stream);
     p.ws = (float*)ws.partial;
+    const int64_t row_tiles = (M * p.G + kGradTile - 1) / kGradTile, key_tiles = (N + kGradTile - 1) / kGradTile;
+    // (before the passes are planned: slices that share a tile's rows stay within 256 workgroups)
+    const bool two = (double)batch * Hq * M * N <= kTwoParts && keys_pass_groups(batch * Hkv * key_tiles, 1) == 2;
     auto pass = [&](bool keys, int64_t tiles, int64_t steps) {
         const FastDiv dt = make_fastdiv((unsigned)tiles);
         p.tiles = (int)tiles;
         p.div_tiles_magic = dt.magic; p.div_tiles_shift = dt.shift;
         p.slices = slices_of(batch * Hkv * tiles, keys ? 256 : 512, steps, 4 * grad_partial(keys, (int)d), ws);
-        return keys ? launch_grad_keys(p, (int)in, (int)d, (hipStream_t)stream) : launch_grad_rows(p, (int)in, (int)d, (hipStream_t)stream);
+        return keys ? launch_grad_keys(p, (int)in, (int)d, two, (hipStream_t)stream) : launch_grad_rows(p, (int)in, (int)d, two, (hipStream_t)stream);
     };
-    const int64_t row_tiles = (M * p.G + kGradTile - 1) / kGradTile, key_tiles = (N + kGradTile - 1) / kGradTile;
     if (!grid_fits(batch * Hkv * row_tiles, kGradThreads) || !grid_fits(batch * Hkv * key_tiles, kGradThreads)) return launch_error(who, hipErrorInvalidConfiguration);
     hipError_t e = hipSuccess;
     if (M > 0) e = pass(false, row_tiles, (N + 63) / 64);

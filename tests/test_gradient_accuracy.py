@@ -120,3 +120,51 @@ def test_a_single_key_has_no_gradient(workspace, lens, dtype, d):  # noqa: F811
             assert torch.all(got["dq"][b] == 0) and torch.all(got["dk"][b] == 0)
             want, mag = do[b].double().sum(0), do[b].double().abs().sum(0)
             assert torch.all((got["dv"][b, 0].double() - want).abs() <= U[dtype] * want.abs() + 1e-5 * mag)
+
+
+# (batch, m, n, key heads, query heads per key head, lens): few probabilities, or up to 16384 of them
+SMALL = [(1, 2, 110, 8, 1, None), (2, 27, 2, 3, 1, [2, 1]), (1, 1, 3, 1, 1, None), (3, 5, 64, 1, 2, [64, 1, 0]), (1, 32, 32, 8, 2, None), (2, 1, 1024, 4, 2, [1024, 300]), (1, 128, 128, 1, 1, None),
+         (16, 1, 64, 16, 1, None), (1, 3, 700, 2, 1, [651]), (1, 1024, 16, 1, 1, None), (1, 1, 500, 1, 8, None)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("shape", SMALL)
+def test_small_calls_round_in_two_parts(workspace, shape, dtype, d):  # noqa: F811
+    """P and dS as operands in two parts leave u^2 of themselves (F16: and 2^-38 of the largest of a row or key); P is within 1e-5 of itself (fp32 scores of up to ten), and D, dP as above:
+    |error| <= u |ref| + |scale| sum (u^2 (|dS| + 4 P A) + 2^-36 max|dS| + 2e-5 P (a + A)) |K|, dK alike, dV: u |ref| + (u^2 + 1e-5) sum P |dO|.  In norm that is the result's own rounding: at most
+    u / sqrt(3) of it if all were just above a power of two, and 1.02 for the rest."""
+    import torch
+    batch, m, n, heads, group, lens = shape
+    g, t, u = torch.Generator().manual_seed(sum(shape[:5]) + d), R.TORCH[dtype], U[dtype]
+    q, do = (torch.randn((batch, m, heads * group, d), generator=g).to(t) for _ in range(2))
+    k, v = (torch.randn((batch, n, heads, d), generator=g).to(t) for _ in range(2))
+    got = _forward_and_backward(q, torch.stack((k, v), 2), do, lens, d ** -0.5, dtype)
+    ref = {x: torch.zeros(y.shape, dtype=torch.float64) for x, y in (("dq", q), ("dk", k), ("dv", v))}
+    tol = {x: torch.zeros_like(y) for x, y in ref.items()}
+    for b in range(batch):
+        length = n if lens is None else lens[b]
+        for j in range(heads * group):
+            h = j // group
+            Q, K, V, G = q[b, :, j].double(), k[b, :length, h].double(), v[b, :length, h].double(), do[b, :, j].double()
+            P = torch.softmax(d ** -0.5 * Q @ K.T, 1) if length else torch.zeros((m, 0), dtype=torch.float64)
+            dP, a = G @ V.T, G.abs() @ V.abs().T
+            A = (P * a).sum(1, keepdim=True)
+            dS = P * (dP - (P * dP).sum(1, keepdim=True))
+            most = float(dS.abs().max()) if length else 0.0
+            fuzz = u * u * (dS.abs() + 4 * P * A) + 2.0 ** -36 * most + 2e-5 * P * (a + A)
+            ref["dq"][b, :, j] = d ** -0.5 * dS @ K
+            tol["dq"][b, :, j] = d ** -0.5 * fuzz @ K.abs()
+            ref["dk"][b, :length, h] += d ** -0.5 * dS.T @ Q
+            tol["dk"][b, :length, h] += d ** -0.5 * fuzz.T @ Q.abs()
+            ref["dv"][b, :length, h] += P.T @ G
+            tol["dv"][b, :length, h] += (u * u + 1e-5) * P.T @ G.abs()
+    worst, norms = {}, {}
+    for x, want in ref.items():
+        err = (got[x].double() - want).abs()
+        worst[x] = float((err / (tol[x] + u * want.abs() + 2.0 ** -25)).max())
+        norms[x] = float(err.norm() / (u * want.norm() + 1e-9 * want.numel() ** 0.5))
+    print(f"[case] small call {shape} {dtype} d={d}: worst of the tolerance {worst}, norms in u {norms}", flush=True)
+    assert max(worst.values()) <= 1, worst
+    assert max(norms.values()) <= 1.02 * 3 ** -0.5, norms
